@@ -279,6 +279,130 @@ int lorc_decode_attn_static(lorc_ctx* ctx, int layer, const lorc_cache* cache, c
 int lorc_decode_step_host(lorc_ctx* ctx, int layer, const lorc_cache* cache, const void* x_host,
                           const void* q_host, void* out_host, int n_splits, void* stream);
 
+/* ---- Uncompressed layers in 8 bits -------------------------------------------------------------------------------
+ * The cache of a FULL layer in 8 bits: the layers that the compression schedule leaves uncompressed take n numbers per
+ * token where the others take r, and soon most of the cache; here such a number takes one byte.  A cached number is
+ * code x scale, with one fp32 scale for every block of LORC_CACHE8_BLOCK tokens and KV head, keys and values apart:
+ *     k, v          codes, rows of n bytes: [batch][seq_stride][n], or paged [n_pages][page_size][n]
+ *     k_scale, ...  [batch][seq_stride / 16][n_kv_heads], or paged [n_pages][page_size / 16][n_kv_heads]
+ * Keys are stored rotated at their positions, as in the bf16 cache of these layers.  page_size and seq_stride are
+ * multiples of 16, so that a block lies within one page.  seq_lens, max_seq_len and the page table are as in lorc_cache.
+ * Attention takes any finite scales; lorc_append8 writes powers of two.  Rows behind a sequence's end, and scales of
+ * blocks wholly behind it, are neither read into a result nor written.
+ * A sequence longer than max_seq_len, the capacity or max_pos counts as empty (status CAPACITY); tokens whose page lies
+ * outside the pool are left out (CAPACITY too).
+ * The calls need a loaded FULL layer and the context's device to be the current one, and like lorc_decode_attn those of one
+ * context must not overlap on the GPU: they share its workspace. */
+#define LORC_CACHE8_INT8 0      /* signed integers from -127 to 127 */
+#define LORC_CACHE8_E4M3 1      /* floating point, 4 exponent and 3 mantissa bits, largest 448 */
+#define LORC_CACHE8_BLOCK 16    /* tokens that share a scale */
+
+typedef struct lorc_cache8 {
+    void* k;                      /* device, 16-byte aligned */
+    void* v;                      /* device, 16-byte aligned */
+    float* k_scale;               /* device */
+    float* v_scale;               /* device */
+    const int32_t* page_table;    /* device, or NULL for the contiguous layout */
+    const int32_t* seq_lens;      /* device */
+    int32_t batch;
+    int32_t max_seq_len;
+    int32_t page_size;            /* paged: tokens per page (multiple of 16) */
+    int32_t max_pages_per_seq;    /* paged */
+    int32_t n_pages;              /* paged: pages in the pool */
+    int32_t type;                 /* LORC_CACHE8_* */
+    int64_t seq_stride;           /* contiguous: rows between consecutive sequences (multiple of 16) */
+} lorc_cache8;
+
+/* Workspace that any of the three calls below needs with the given sizes; T: the most new tokens per sequence of a call.
+ * 0 for sizes that are not positive. */
+size_t lorc_cache8_workspace_bytes(const lorc_ctx* ctx, int batch, int max_seq_len, int T);
+
+/* Cache write: RoPE(x W_k) and x W_v of T new tokens per sequence, x and positions as in lorc_append, in fp32 until they
+ * are rounded to codes (to nearest, ties to even).  The scale of a block and head becomes the smallest power of two 2^e,
+ * -100 <= e <= 100, with which no new number exceeds the largest code (127, or 448), or stays what it is if the block holds
+ * earlier tokens of the sequence under a larger one.  Where it grows, the codes of these are re-expressed under the new
+ * scale (e4m3: exactly, down to its subnormal numbers; int8: one more rounding, half a step at most, and none unless the
+ * scale doubles).  A NaN is stored as 0 and an infinity as the largest code; neither counts for the scale, and the status
+ * becomes ARG.
+ * Errors: ARG, LAYER, UNSUPPORTED (a compressed layer), WORKSPACE; CAPACITY through the status word. */
+int lorc_append8(lorc_ctx* ctx, int layer, const lorc_cache8* cache, const void* x, int T, void* stream);
+
+/* Decode attention, as lorc_decode_attn, over the 8-bit cache.  q, out [batch, n_q_heads, d_head] bf16.  The work of all
+ * sequences is dealt out evenly to the blocks that the GPU holds at once, whatever the lengths are; the lengths and the GPU's
+ * number of SMs decide the order of sums.  Status EMPTY and a row of zeros for a sequence without tokens.
+ * Errors: ARG, LAYER, UNSUPPORTED (a compressed layer), WORKSPACE; CAPACITY / EMPTY through the status word. */
+int lorc_decode_attn8(lorc_ctx* ctx, int layer, const lorc_cache8* cache, const void* q, void* out, void* stream);
+
+/* Attention of the T newest tokens of every sequence, as lorc_prefill_attn, over the 8-bit cache: q, out
+ * [batch, T, n_q_heads, d_head] bf16; the T tokens are already cached, and query t sees the tokens up to its own.  A
+ * sequence with fewer than T tokens gets zeros, and status ARG (EMPTY if it has none).  With the head geometries of the
+ * tcgen05 kernels keys and values are brought to fp16 in the workspace once per call (code x scale must stay below 65504;
+ * tokens whose page lies outside the pool count as zeros there).
+ * Errors: ARG, LAYER, UNSUPPORTED (a compressed layer), WORKSPACE; CAPACITY / EMPTY / ARG through the status word. */
+int lorc_prefill_attn8(lorc_ctx* ctx, int layer, const lorc_cache8* cache, const void* q, void* out, int T, void* stream);
+
+/* ---- Pages ---------------------------------------------------------------------------------------------------------
+ * Sequences that share, take and give back pages of a pool, on the device (so that a captured step may do it) and for
+ * any of the caches above: a pool is a set of arrays with one entry per page, such as the latents C_K and C_V of every
+ * layer (page_bytes = page_size * r * 2), or codes and scales of every 8-bit cache.  All arrays share page numbers,
+ * page table and lengths.
+ * refs[p] counts the rows of the page table that hold page p; a page with refs[p] = 0 is free.  Row s holds the pages
+ * page_table[s][0 .. ceil(seq_lens[s] / page_size) - 1]; its other entries mean nothing.  (A negative length counts as 0.)
+ * Pages that a call takes are the lowest free ones, in the order in which the call lists who needs them.
+ * A table entry outside the pool, or a length beyond max_pages_per_seq * page_size, sets status CAPACITY; the entry is
+ * left out, and the row of such a length neither forks nor grows.
+ * Plans live in the context's workspace (lorc_pages_workspace_bytes); calls on one context must not overlap on the GPU.
+ * The calls use no factors: any context will do. */
+typedef struct lorc_page_buf {
+    void* base;                   /* device, 4-byte aligned: page p starts at base + p * page_bytes */
+    int64_t page_bytes;           /* positive multiple of 4, at most 2^32; multiples of 16 on a 16-byte aligned base copy faster */
+} lorc_page_buf;
+
+typedef struct lorc_pages {
+    const lorc_page_buf* bufs;    /* host array, read during the call */
+    int32_t n_bufs;               /* at most LORC_PAGES_MAX_BUFS */
+    int32_t n_pages;
+    int32_t page_size;            /* tokens per page */
+    int32_t max_pages_per_seq;
+    int32_t n_rows;               /* rows of page_table, entries of seq_lens */
+    int32_t reserved;
+    int32_t* page_table;          /* device [n_rows][max_pages_per_seq] */
+    int32_t* seq_lens;            /* device [n_rows] */
+    int32_t* refs;                /* device [n_pages] */
+} lorc_pages;
+
+#define LORC_PAGES_MAX_BUFS 1024
+#define LORC_PAGES_MAX_LIST 65536
+
+/* Workspace that any of the calls below needs; n: the longest list of a call (fork: pairs, free: rows). */
+size_t lorc_pages_workspace_bytes(const lorc_pages* pages, int n);
+
+/* Rows rows[i] (device int32 [n]) give their pages back: refs of each falls by one, the length becomes 0.  The table's
+ * entries stay as they are.  A row that is listed twice, or empty, gives back nothing more; one outside the table sets
+ * status ARG. */
+int lorc_pages_free(lorc_ctx* ctx, const lorc_pages* pages, const int32_t* rows, int n, void* stream);
+
+/* Row children[i] becomes a copy of row parents[i] (device int32 [n]): it holds the same full pages (refs of each grows
+ * by one) and, where the parent's last page is partly filled, a page of its own with that page's contents, in every array;
+ * and it has the parent's length.  So parent and child can both be written to.  The parent's row stays as it is, and may be
+ * listed more than once.  A pair is left out, with status ARG, if a row is outside the table, the child is not empty, or
+ * the child stands earlier in the list; and with status CAPACITY, its child staying empty, if no free page is left for it. */
+int lorc_pages_fork(lorc_ctx* ctx, const lorc_pages* pages, const int32_t* parents, const int32_t* children, int n, void* stream);
+
+/* Room for grow[s] more tokens (device int32 [n_rows], <= 0: none) in every row s: takes the pages that this needs, in the
+ * order of the rows, and raises seq_lens[s] by grow[s], as lorc_append expects it.  A row that does not fit the table or
+ * for which there are too few free pages is left as it is, with status CAPACITY; such a row's demand is not handed to the
+ * rows behind it.  (A partly filled last page is taken to be the row's own, as fork leaves it.) */
+int lorc_pages_grow(lorc_ctx* ctx, const lorc_pages* pages, const int32_t* grow, void* stream);
+
+/* Moves the used pages to the front: with u pages used, those numbered u and above move, in ascending order, to the free
+ * pages below u, in ascending order, in every array; refs and the rows' entries follow.  page_table_out and refs_out
+ * receive the new table and counts (NULL: in place); entries that hold no page are copied as they are.  With tables of
+ * their own the old ones stay valid, and the moved pages keep their contents, until one of these pages is taken again.
+ * n_used (device int32, or NULL) receives u. */
+int lorc_pages_compact(lorc_ctx* ctx, const lorc_pages* pages, int32_t* page_table_out, int32_t* refs_out, int32_t* n_used,
+                       void* stream);
+
 /* Synchronise `stream`, then read and clear the device status word.  Returns
  * LORC_OK or the first error a kernel recorded since the last call. */
 int lorc_sync_status(lorc_ctx* ctx, void* stream);

@@ -32,6 +32,11 @@ LORC_FLAG_PROFILE = 2
 LORC_N_STAGES = 4
 LORC_STAGE_NAMES = ("append", "score", "pv", "combine")
 LORC_STATIC_SCRATCH_BYTES = 8 << 20
+LORC_CACHE8_INT8 = 0
+LORC_CACHE8_E4M3 = 1
+LORC_CACHE8_BLOCK = 16
+LORC_PAGES_MAX_BUFS = 1024
+LORC_PAGES_MAX_LIST = 65536
 
 
 class lorc_model_desc(C.Structure):
@@ -51,6 +56,29 @@ class lorc_cache(C.Structure):
     ]
 
 
+class lorc_cache8(C.Structure):
+    _fields_ = [
+        ("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+        ("page_table", C.c_void_p), ("seq_lens", C.c_void_p),
+        ("batch", C.c_int32), ("max_seq_len", C.c_int32), ("page_size", C.c_int32),
+        ("max_pages_per_seq", C.c_int32), ("n_pages", C.c_int32), ("type", C.c_int32),
+        ("seq_stride", C.c_int64),
+    ]
+
+
+class lorc_page_buf(C.Structure):
+    _fields_ = [("base", C.c_void_p), ("page_bytes", C.c_int64)]
+
+
+class lorc_pages(C.Structure):
+    _fields_ = [
+        ("bufs", C.POINTER(lorc_page_buf)),
+        ("n_bufs", C.c_int32), ("n_pages", C.c_int32), ("page_size", C.c_int32),
+        ("max_pages_per_seq", C.c_int32), ("n_rows", C.c_int32), ("reserved", C.c_int32),
+        ("page_table", C.c_void_p), ("seq_lens", C.c_void_p), ("refs", C.c_void_p),
+    ]
+
+
 class LorcError(RuntimeError):
     def __init__(self, code, msg):
         super().__init__(f"lorc error {code}: {msg}")
@@ -60,6 +88,8 @@ class LorcError(RuntimeError):
 def _signatures():
     vp, i32, i64 = C.c_void_p, C.c_int, C.c_int64
     cp = C.POINTER(lorc_cache)
+    c8 = C.POINTER(lorc_cache8)
+    pg = C.POINTER(lorc_pages)
     return {
         "lorc_create": ([C.POINTER(lorc_model_desc), C.POINTER(vp)], i32),
         "lorc_destroy": ([vp], i32),
@@ -76,6 +106,15 @@ def _signatures():
         "lorc_merge_shards": ([vp, i32, vp, vp, vp, i32, vp], i32),
         "lorc_decode_attn_static": ([vp, i32, cp, vp, vp, i32, vp], i32),
         "lorc_decode_step_host": ([vp, i32, cp, vp, vp, vp, i32, vp], i32),
+        "lorc_cache8_workspace_bytes": ([vp, i32, i32, i32], C.c_size_t),
+        "lorc_append8": ([vp, i32, c8, vp, i32, vp], i32),
+        "lorc_decode_attn8": ([vp, i32, c8, vp, vp, vp], i32),
+        "lorc_prefill_attn8": ([vp, i32, c8, vp, vp, i32, vp], i32),
+        "lorc_pages_workspace_bytes": ([pg, i32], C.c_size_t),
+        "lorc_pages_free": ([vp, pg, vp, i32, vp], i32),
+        "lorc_pages_fork": ([vp, pg, vp, vp, i32, vp], i32),
+        "lorc_pages_grow": ([vp, pg, vp, vp], i32),
+        "lorc_pages_compact": ([vp, pg, vp, vp, vp, vp], i32),
         "lorc_sync_status": ([vp, vp], i32),
         "lorc_last_error": ([vp], C.c_char_p),
         "lorc_last_path": ([vp], i32),
@@ -227,6 +266,68 @@ def lorc_decode_step_host(ctx, layer, cache, x_host, q_host, out_host, n_splits=
 
 def lorc_selftest_wait_expiry(ctx, limit_ns, stream=None):
     _check(ctx, _lib.lorc_selftest_wait_expiry(ctx, int(limit_ns), _stream(stream)))
+
+
+def make_cache8(k, v, k_scale, v_scale, seq_lens, batch, max_seq_len, type, page_table=None, page_size=0, max_pages_per_seq=0,
+                n_pages=0, seq_stride=0):
+    """Fill a lorc_cache8 descriptor from tensors (pointers only; nothing is copied)."""
+    return lorc_cache8(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _ptr(page_table), _ptr(seq_lens), batch, max_seq_len,
+                       page_size, max_pages_per_seq, n_pages, type, seq_stride)
+
+
+def lorc_cache8_workspace_bytes(ctx, batch, max_seq_len, T=1):
+    return int(_lib.lorc_cache8_workspace_bytes(ctx, batch, max_seq_len, T))
+
+
+def lorc_append8(ctx, layer, cache, x, T=1, stream=None):
+    _check(ctx, _lib.lorc_append8(ctx, layer, C.byref(cache), _ptr(x), T, _stream(stream)))
+
+
+def lorc_decode_attn8(ctx, layer, cache, q, out, stream=None):
+    _check(ctx, _lib.lorc_decode_attn8(ctx, layer, C.byref(cache), _ptr(q), _ptr(out), _stream(stream)))
+
+
+def lorc_prefill_attn8(ctx, layer, cache, q, out, T, stream=None):
+    _check(ctx, _lib.lorc_prefill_attn8(ctx, layer, C.byref(cache), _ptr(q), _ptr(out), T, _stream(stream)))
+
+
+def make_pages(bufs, page_table, seq_lens, refs, page_size):
+    """Fill a lorc_pages descriptor from tensors (pointers only; nothing is copied).  bufs: the pool's arrays, contiguous
+    tensors whose first dimension is the page; page_table [rows, pages per row], seq_lens [rows], refs [pages]: int32."""
+    n_pages = refs.numel()
+    for t in bufs:
+        if t.shape[0] != n_pages or not t.is_contiguous():
+            raise ValueError("make_pages: an array of the pool is not contiguous, or has another number of pages than refs")
+    for t in (page_table, seq_lens, refs):
+        if t.element_size() != 4 or t.is_floating_point() or not t.is_contiguous():
+            raise ValueError("make_pages: page table, lengths and counts are contiguous int32 tensors")
+    if page_table.dim() != 2 or seq_lens.numel() != page_table.shape[0]:
+        raise ValueError("make_pages: the page table has a row for every length")
+    arr = (lorc_page_buf * max(1, len(bufs)))(
+        *[lorc_page_buf(_ptr(t), t.numel() // n_pages * t.element_size()) for t in bufs])
+    return lorc_pages(arr, len(bufs), n_pages, page_size, page_table.shape[1], page_table.shape[0], 0, _ptr(page_table),
+                      _ptr(seq_lens), _ptr(refs))
+
+
+def lorc_pages_workspace_bytes(pages, n):
+    return int(_lib.lorc_pages_workspace_bytes(C.byref(pages), n))
+
+
+def lorc_pages_free(ctx, pages, rows, n, stream=None):
+    _check(ctx, _lib.lorc_pages_free(ctx, C.byref(pages), _ptr(rows), n, _stream(stream)))
+
+
+def lorc_pages_fork(ctx, pages, parents, children, n, stream=None):
+    _check(ctx, _lib.lorc_pages_fork(ctx, C.byref(pages), _ptr(parents), _ptr(children), n, _stream(stream)))
+
+
+def lorc_pages_grow(ctx, pages, grow, stream=None):
+    _check(ctx, _lib.lorc_pages_grow(ctx, C.byref(pages), _ptr(grow), _stream(stream)))
+
+
+def lorc_pages_compact(ctx, pages, page_table_out=None, refs_out=None, n_used=None, stream=None):
+    _check(ctx, _lib.lorc_pages_compact(ctx, C.byref(pages), _ptr(page_table_out), _ptr(refs_out), _ptr(n_used),
+                                         _stream(stream)))
 
 
 def lorc_sync_status(ctx, stream=None):

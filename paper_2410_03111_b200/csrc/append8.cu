@@ -1,0 +1,281 @@
+// Cache write of uncompressed layers in 8 bits: [K | V] = x [W_k | W_v], keys rotated, both rounded to codes with one scale per
+// block of 16 tokens and KV head.
+//
+// Two kernels.  The projection leaves fp32 numbers [tokens][2 n] in the workspace; the second kernel has a block of threads for each
+// (block of tokens, KV head, keys or values), which sees all numbers that share a scale.
+#include <math.h>
+
+#include "cache8.cuh"
+#include "sm100_ptx.cuh"
+#include "tc_kernels.cuh"
+
+using namespace sm100;
+
+namespace {
+
+// ---------------------------------------------------------------------------------------------
+// projection for a handful of tokens: grid (2 n / 8, tiles of 16 tokens), eight warps = eight slices of D.  Bound by the stream of
+// the factor (in fragment order, see retile_factor_kernel), which is requested before the kernel in front has finished.
+// ---------------------------------------------------------------------------------------------
+__global__ void __launch_bounds__(256, 2)
+project8_mma_kernel(const bf16* __restrict__ x, const bf16* __restrict__ A_tiled, float* __restrict__ proj, int D, int R,
+                    long long n_tok) {
+    __shared__ float red[8][32][4];
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+    const int g = lane >> 2, t = lane & 3;
+    const int n0 = blockIdx.x * 8;
+    const long long m0 = (long long)blockIdx.y * 16;
+    const int kspan = D / 8, k_begin = warp * kspan, steps = kspan / 32;
+    const bool row_lo = m0 + g < n_tok, row_hi = m0 + g + 8 < n_tok;
+    const uint4* xa = reinterpret_cast<const uint4*>(x + (m0 + g) * D + k_begin) + t;
+    const uint4* xb = reinterpret_cast<const uint4*>(x + (m0 + g + 8) * D + k_begin) + t;
+    const uint4* wb = reinterpret_cast<const uint4*>(A_tiled) + ((long long)blockIdx.x * (D / 32) + k_begin / 32) * 32 + lane;
+    const uint4 zero = make_uint4(0, 0, 0, 0);
+    float c[4] = {0.f, 0.f, 0.f, 0.f};
+    uint4 w[16];
+    auto load_factor = [&](int kb0) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            w[i] = zero;
+            if (kb0 + i < steps)
+                asm volatile("ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];"
+                             : "=r"(w[i].x), "=r"(w[i].y), "=r"(w[i].z), "=r"(w[i].w)
+                             : "l"(wb + (kb0 + i) * 32));
+        }
+    };
+    load_factor(0);
+    grid_dep_wait();
+    grid_dep_launch();
+    for (int kb0 = 0; kb0 < steps; kb0 += 16) {
+        if (kb0 > 0) load_factor(kb0);
+#pragma unroll
+        for (int i0 = 0; i0 < 16; i0 += 4) {
+            uint4 lo[4], hi[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                lo[i] = zero;
+                hi[i] = zero;
+                if (kb0 + i0 + i < steps) {
+                    if (row_lo) lo[i] = xa[(kb0 + i0 + i) * 4];
+                    if (row_hi) hi[i] = xb[(kb0 + i0 + i) * 4];
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (kb0 + i0 + i < steps) {
+                    mma_bf16_16816(c, lo[i].x, hi[i].x, lo[i].y, hi[i].y, w[i0 + i].x, w[i0 + i].y);
+                    mma_bf16_16816(c, lo[i].z, hi[i].z, lo[i].w, hi[i].w, w[i0 + i].z, w[i0 + i].w);
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) red[warp][lane][i] = c[i];
+    __syncthreads();
+    if (warp != 0) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        c[i] = ((red[0][lane][i] + red[1][lane][i]) + (red[2][lane][i] + red[3][lane][i])) +
+               ((red[4][lane][i] + red[5][lane][i]) + (red[6][lane][i] + red[7][lane][i]));
+    const int col = n0 + 2 * t;
+    if (row_lo) *reinterpret_cast<float2*>(proj + (m0 + g) * R + col) = make_float2(c[0], c[1]);
+    if (row_hi) *reinterpret_cast<float2*>(proj + (m0 + g + 8) * R + col) = make_float2(c[2], c[3]);
+}
+
+// The same without conditions on D: thread = column, eight tokens, columns of W as they are.
+__global__ void __launch_bounds__(128)
+project8_plain_kernel(const bf16* __restrict__ x, const bf16* __restrict__ A_cat, float* __restrict__ proj, int D, int R,
+                      long long n_tok) {
+    constexpr int TT = 8, CH = 512;
+    __shared__ float xs[TT][CH];
+    const int tid = threadIdx.x, col = blockIdx.x * 128 + tid;
+    const long long tok0 = (long long)blockIdx.y * TT;
+    float acc[TT];
+#pragma unroll
+    for (int t = 0; t < TT; ++t) acc[t] = 0.f;
+    grid_dep_wait();
+    grid_dep_launch();
+    for (int d0 = 0; d0 < D; d0 += CH) {
+        const int dn = min(CH, D - d0);
+        for (int i = tid; i < TT * CH; i += 128) {
+            const int t = i / CH, d = i - t * CH;
+            xs[t][d] = tok0 + t < n_tok && d < dn ? __bfloat162float(x[(tok0 + t) * D + d0 + d]) : 0.f;
+        }
+        __syncthreads();
+        if (col < R)
+            for (int d = 0; d < dn; ++d) {
+                const float a = __bfloat162float(A_cat[(long long)(d0 + d) * R + col]);
+#pragma unroll
+                for (int t = 0; t < TT; ++t) acc[t] = fmaf(xs[t][d], a, acc[t]);
+            }
+        __syncthreads();
+    }
+    if (col < R)
+#pragma unroll
+        for (int t = 0; t < TT; ++t)
+            if (tok0 + t < n_tok) proj[(tok0 + t) * R + col] = acc[t];
+}
+
+// ---------------------------------------------------------------------------------------------
+// rotation and quantisation: grid (batch * blocks a chunk can reach, KV heads, keys / values); 16 threads of 16 bytes per row of 128
+// dimensions are eight, so 128 (64) threads are the 16 rows.  A thread owns 16 dimensions of a row: one 16-byte store.
+// ---------------------------------------------------------------------------------------------
+struct Quant8Params {
+    const float* proj;
+    Cache8View cv;
+    const float2* rope_table;
+    int* status;
+    int T, n_blocks, max_pos, interleaved, pairs_adjacent;     // pairs_adjacent: see the key columns of retile_factor_kernel
+};
+
+template <int DH, bool E4M3>
+__global__ void __launch_bounds__(DH)
+quantize8_kernel(const Quant8Params p) {
+    constexpr int TPR = DH / 16, WARPS = DH / 32;
+    __shared__ float most_s[WARPS];
+    __shared__ int flags_s[WARPS];
+    const Cache8View& cv = p.cv;
+    const int tid = threadIdx.x, r = tid / TPR, d0 = (tid % TPR) * 16;
+    const int s = (int)blockIdx.x / p.n_blocks, head = blockIdx.y;
+    const bool val = blockIdx.z != 0;
+    grid_dep_wait();
+    grid_dep_launch();
+    const int len = cv.seq_lens[s], first = len - p.T;
+    // a sequence that is too long, or shorter than what is written to it, is reported; of the latter the tokens that have a place
+    // are written
+    const bool fits = len <= cv.max_seq_len && len <= p.max_pos && len <= cv.capacity;
+    if ((!fits || first < 0) && tid == 0) lorc_set_status(p.status, LORC_ERR_CAPACITY);
+    if (!fits) return;
+    const int begin = max(first, 0);
+    const int blk = begin / LORC_BLOCK8 + (int)blockIdx.x % p.n_blocks;
+    if (blk * LORC_BLOCK8 >= len) return;
+    const long long at = lorc_block8(cv, s, blk);
+    if (at < 0) {
+        if (tid == 0) lorc_set_status(p.status, LORC_ERR_CAPACITY);
+        return;
+    }
+    const int pos = blk * LORC_BLOCK8 + r;
+    const bool fresh = pos >= begin && pos < len, old = pos < begin;
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = 0.f;
+    if (fresh) {
+        const float* src = p.proj + ((long long)s * p.T + (pos - first)) * (2 * cv.n) + (val ? cv.n : 0) + head * DH;
+        if (val) {
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) *reinterpret_cast<float4*>(x + i) = *reinterpret_cast<const float4*>(src + d0 + i);
+        } else {
+            const float2* cs = p.rope_table + (long long)pos * (DH / 2);
+            if (p.interleaved) {
+#pragma unroll
+                for (int i = 0; i < 16; i += 2) {
+                    const float2 ab = *reinterpret_cast<const float2*>(src + d0 + i), c = cs[(d0 + i) / 2];
+                    x[i] = ab.x * c.x - ab.y * c.y;
+                    x[i + 1] = ab.x * c.y + ab.y * c.x;
+                }
+            } else {
+                const bool second = d0 >= DH / 2;
+                const int j0 = second ? d0 - DH / 2 : d0;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int j = j0 + i;
+                    const float a = src[p.pairs_adjacent ? 2 * j : j], b = src[p.pairs_adjacent ? 2 * j + 1 : j + DH / 2];
+                    const float2 c = cs[j];
+                    x[i] = second ? a * c.y + b * c.x : a * c.x - b * c.y;
+                }
+            }
+        }
+    }
+    // largest magnitude of the new numbers; what is not finite does not count
+    float most = 0.f;
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const float m = fabsf(x[i]);
+        if (m <= 3.4028234663852886e38f) most = fmaxf(most, m);
+        else odd = true;
+    }
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+    const int any_odd = __any_sync(0xffffffffu, odd);
+    if ((tid & 31) == 0) {
+        most_s[tid >> 5] = most;
+        flags_s[tid >> 5] = any_odd;
+    }
+    // the scale so far, where earlier tokens stand under it.  (Read by all threads before the barrier, written by one behind it.)
+    float* scale_at = (val ? cv.v_scale : cv.k_scale) + at * cv.n_kv + head;
+    float before = begin > blk * LORC_BLOCK8 ? *scale_at : 0.f;
+    before = before > 0.f ? before : 0.f;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) most = fmaxf(most, most_s[w]);
+    int bad = 0;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) bad |= flags_s[w];
+    const float scale = fmaxf(lorc_scale8<E4M3>(most), before);
+    if (tid == 0) {
+        *scale_at = scale;
+        if (bad) lorc_set_status(p.status, LORC_ERR_ARG);
+    }
+    uint4* dst = reinterpret_cast<uint4*>((val ? cv.v : cv.k) + (at * LORC_BLOCK8 + r) * cv.n + head * DH + d0);
+    uint32_t w[4];
+    if (fresh) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            w[i] = lorc_to_codes2<E4M3>(x[4 * i] / scale, x[4 * i + 1] / scale) |
+                   lorc_to_codes2<E4M3>(x[4 * i + 2] / scale, x[4 * i + 3] / scale) << 16;
+        *dst = make_uint4(w[0], w[1], w[2], w[3]);
+    } else if (old && scale != before) {
+        const float keep = before / scale;
+        const uint4 c = *dst;
+        const uint32_t in[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t a, b;
+            lorc_codes_half<E4M3, 0, 1, 2, 3>(in[i], a, b);
+            const float2 u = __half22float2(*reinterpret_cast<__half2*>(&a)), v = __half22float2(*reinterpret_cast<__half2*>(&b));
+            w[i] = lorc_to_codes2<E4M3>(u.x * keep, u.y * keep) | lorc_to_codes2<E4M3>(v.x * keep, v.y * keep) << 16;
+        }
+        *dst = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+}  // namespace
+
+size_t lorc_append8_scratch_bytes(const lorc_ctx* ctx, int batch, int T) {
+    return lorc_align_up((size_t)batch * T * 2 * ctx->n * sizeof(float), 256);
+}
+
+cudaError_t lorc_append8_launch(lorc_ctx* ctx, const LorcLayer& L, const Cache8View& cv, const bf16* x, int T, void* scratch,
+                                cudaStream_t st, int* launches) {
+    const int D = ctx->desc.d_model, R = 2 * ctx->n;
+    const long long n_tok = (long long)cv.batch * T;
+    float* proj = (float*)scratch;
+    const bool mma = D % 256 == 0 && L.A_tiled != nullptr;
+    // grid rows are limited to 65535: chunks of as many tokens
+    const int tile = mma ? 16 : 8;
+    const long long most = 65535ll * tile;
+    for (long long t0 = 0; t0 < n_tok; t0 += most) {
+        const long long cnt = n_tok - t0 < most ? n_tok - t0 : most;
+        const unsigned y = (unsigned)((cnt + tile - 1) / tile);
+        cudaError_t e =
+            mma ? lorc_launch_dependent(project8_mma_kernel, dim3(R / 8, y), dim3(256), 0, st, x + t0 * D, (const bf16*)L.A_tiled,
+                                        proj + t0 * R, D, R, cnt)
+                : lorc_launch_dependent(project8_plain_kernel, dim3((R + 127) / 128, y), dim3(128), 0, st, x + t0 * D,
+                                        (const bf16*)L.A_cat, proj + t0 * R, D, R, cnt);
+        *launches += 1;
+        if (e != cudaSuccess) return e;
+    }
+    Quant8Params p;
+    p.proj = proj; p.cv = cv; p.rope_table = ctx->rope_table; p.status = ctx->status_dev; p.T = T; p.max_pos = ctx->desc.max_pos;
+    p.n_blocks = (T + LORC_BLOCK8 - 2) / LORC_BLOCK8 + 1;
+    p.interleaved = ctx->pair_style == LORC_ROPE_INTERLEAVED;
+    p.pairs_adjacent = mma && ctx->pair_style == LORC_ROPE_HALF_SPLIT;
+    const dim3 grid((unsigned)((long long)cv.batch * p.n_blocks), (unsigned)cv.n_kv, 2);
+    const int DH = ctx->desc.d_head;
+    const bool e4m3 = cv.type == LORC_CACHE8_E4M3;
+    auto kernel = DH == 128 ? (e4m3 ? quantize8_kernel<128, true> : quantize8_kernel<128, false>)
+                            : (e4m3 ? quantize8_kernel<64, true> : quantize8_kernel<64, false>);
+    *launches += 1;
+    return lorc_launch_dependent(kernel, grid, dim3(DH), 0, st, p);
+}

@@ -1,0 +1,105 @@
+// Prompt chunks over the 8-bit cache of uncompressed layers: keys and values of the cached tokens are brought to fp16 once per
+// call (code x scale: seven significant bits, exact unless the scale is no power of two), then the tcgen05 attention kernel of the
+// latent mode runs over them.  With T queries per sequence that kernel does 4 T d G products per number of the buffer, so the
+// pass over it is small for chunks; a call with few queries is better served by the streaming kernel.
+#include <math.h>
+
+#include "cache8.cuh"
+#include "sm100_ptx.cuh"
+#include "tc_kernels.cuh"
+
+using namespace sm100;
+
+namespace {
+
+struct Expand8Params {
+    Cache8View cv;
+    uint4 *khat, *vbuf;              // [batch][rows][n] fp16
+    int* status;
+    long long rows;
+    int dh_shift, max_pos, T;
+};
+
+// A block of threads per (block of 16 tokens, keys / values): 16 codes per thread and step.  Rows of the buffer behind the
+// sequence's end, up to a multiple of 128, become zero: the attention kernel reads whole tiles.
+template <bool E4M3>
+__global__ void __launch_bounds__(256)
+expand8_kernel(const Expand8Params p) {
+    const Cache8View& cv = p.cv;
+    const int blk = blockIdx.x, s = blockIdx.y;
+    const bool val = blockIdx.z != 0;
+    grid_dep_wait();
+    grid_dep_launch();
+    const int len = cv.seq_lens[s];
+    // (what the attention kernel treats as empty has no rows to read)
+    if (len < p.T || len > cv.max_seq_len || len > p.max_pos) return;
+    if (blk * LORC_BLOCK8 >= (len + 127) / 128 * 128) return;
+    long long at = -1;
+    if (blk * LORC_BLOCK8 < len) {
+        at = lorc_block8(cv, s, blk);
+        if (at < 0 && threadIdx.x == 0) lorc_set_status(p.status, LORC_ERR_CAPACITY);
+    }
+    const int per_row = cv.n / 16;                               // pieces of 16 codes
+    const uint4* src = reinterpret_cast<const uint4*>(val ? cv.v : cv.k) + at * LORC_BLOCK8 * per_row;
+    const float* scale = (val ? cv.v_scale : cv.k_scale) + at * cv.n_kv;
+    uint4* dst = (val ? p.vbuf : p.khat) + ((long long)s * p.rows + (long long)blk * LORC_BLOCK8) * per_row * 2;
+    for (int i = threadIdx.x; i < LORC_BLOCK8 * per_row; i += 256) {
+        const int r = i / per_row, c = i - r * per_row;
+        uint4 lo = make_uint4(0u, 0u, 0u, 0u), hi = lo;
+        if (at >= 0 && blk * LORC_BLOCK8 + r < len) {
+            const uint4 x = src[i];
+            const float f = scale[(c * 16) >> p.dh_shift];
+            const uint32_t in[4] = {x.x, x.y, x.z, x.w};
+            uint32_t w[8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                uint32_t a, b;
+                lorc_codes_half<E4M3, 0, 1, 2, 3>(in[j], a, b);
+                const float2 u = __half22float2(*reinterpret_cast<__half2*>(&a)), v = __half22float2(*reinterpret_cast<__half2*>(&b));
+                const __half2 y = __floats2half2_rn(u.x * f, u.y * f), z = __floats2half2_rn(v.x * f, v.y * f);
+                w[2 * j] = *reinterpret_cast<const uint32_t*>(&y);
+                w[2 * j + 1] = *reinterpret_cast<const uint32_t*>(&z);
+            }
+            lo = make_uint4(w[0], w[1], w[2], w[3]);
+            hi = make_uint4(w[4], w[5], w[6], w[7]);
+        }
+        dst[2 * i] = lo;
+        dst[2 * i + 1] = hi;
+    }
+}
+
+size_t expand8_rows(int max_seq_len) { return ((size_t)max_seq_len + 127) / 128 * 128; }
+
+}  // namespace
+
+bool lorc_prefill8_supported(const lorc_ctx* ctx) {
+    return lorc_tc_prefill_shape_ok(ctx) && !(ctx->desc.flags & LORC_FLAG_DEBUG_FP32) && lorc_get_tmap_encode() != nullptr;
+}
+
+size_t lorc_prefill8_scratch_bytes(const lorc_ctx* ctx, int batch, int max_seq_len) {
+    return 2 * lorc_align_up((size_t)batch * expand8_rows(max_seq_len) * ctx->n * 2, 256);
+}
+
+cudaError_t lorc_prefill8_launch(lorc_ctx* ctx, const Cache8View& cv, const bf16* q, bf16* out, int T, void* scratch,
+                                 cudaStream_t st, int* launches) {
+    static bool attr[64] = {false};
+    const bool known = ctx->device >= 0 && ctx->device < 64;
+    cudaError_t e = cudaSuccess;
+    if (!known || !attr[ctx->device]) {
+        e = lorc_tc_prefill_set_attrs();
+        if (e != cudaSuccess) return e;
+        if (known) attr[ctx->device] = true;
+    }
+    const size_t rows = expand8_rows(cv.max_seq_len);
+    Expand8Params p;
+    p.cv = cv; p.status = ctx->status_dev; p.rows = (long long)rows; p.max_pos = ctx->desc.max_pos; p.T = T;
+    p.khat = (uint4*)scratch;
+    p.vbuf = (uint4*)((char*)scratch + lorc_prefill8_scratch_bytes(ctx, cv.batch, cv.max_seq_len) / 2);
+    p.dh_shift = ctx->desc.d_head == 128 ? 7 : 6;
+    const dim3 grid((unsigned)(rows / LORC_BLOCK8), (unsigned)cv.batch, 2);
+    e = cv.type == LORC_CACHE8_E4M3 ? lorc_launch_dependent(expand8_kernel<true>, grid, dim3(256), 0, st, p)
+                                    : lorc_launch_dependent(expand8_kernel<false>, grid, dim3(256), 0, st, p);
+    *launches += 1;
+    if (e != cudaSuccess) return e;
+    return lorc_tc_prefill_attend(ctx, cv.seq_lens, cv.batch, rows, cv.max_seq_len, p.khat, p.vbuf, q, out, T, st, launches);
+}

@@ -97,6 +97,10 @@ cudaError_t lorc_tc_prefill_set_attrs();
 cudaError_t lorc_tc_prefill_launch(lorc_ctx* ctx, const LorcLayer& L, const CacheView& cv, const CUtensorMap& mapCK,
                                    const CUtensorMap& mapCV, const CUtensorMap* mapBKT, const CUtensorMap* mapBVT,
                                    const bf16* q, bf16* out, int T, void* scratch, cudaStream_t st, int* launches);
+// Its second half: the attention over keys (rotated) and values [batch, rows, n] in fp16, rows a multiple of 128.  A
+// sequence of more than max_len tokens is treated as empty (and reported).
+cudaError_t lorc_tc_prefill_attend(lorc_ctx* ctx, const int32_t* seq_lens, int batch, size_t rows, int max_len, const void* khat,
+                                   const void* vbuf, const bf16* q, bf16* out, int T, cudaStream_t st, int* launches);
 cudaError_t lorc_tc_prefill(lorc_ctx* ctx, int layer, const LorcLayer& L, const CacheView& cv, const bf16* q, bf16* out,
                             int T, void* ws, size_t ws_bytes, cudaStream_t st, int* launches);
 

@@ -691,6 +691,35 @@ cudaError_t lorc_tc_prefill_set_attrs() {
     return e;
 }
 
+// keys or values [batch, rows, n] fp16 in swizzled boxes of 64 columns x 128 rows
+static bool prefill_kv_map(const lorc_ctx* ctx, const void* base, int batch, size_t rows, CUtensorMap* map) {
+    uint64_t kd[3] = {(uint64_t)ctx->n, (uint64_t)rows, (uint64_t)batch};
+    uint64_t ks[2] = {(uint64_t)ctx->n * 2, (uint64_t)rows * ctx->n * 2};
+    uint32_t kb[3] = {KC, TILE, 1};
+    return lorc_make_tmap_bf16(map, base, 3, kd, ks, kb);
+}
+
+cudaError_t lorc_tc_prefill_attend(lorc_ctx* ctx, const int32_t* seq_lens, int batch, size_t rows, int max_len, const void* khat, const void* vbuf,
+                                   const bf16* q, bf16* out, int T, cudaStream_t st, int* launches) {
+    const lorc_model_desc& d = ctx->desc;
+    CUtensorMap mapQ, mapK, mapV;
+    {
+        // q [b, T, H_q, 128]: box = 64 elements x G heads x 128 / G positions
+        uint64_t dims[4] = {128, (uint64_t)d.n_q_heads, (uint64_t)T, (uint64_t)batch};
+        uint64_t str[3] = {128 * 2, (uint64_t)d.n_q_heads * 128 * 2, (uint64_t)T * d.n_q_heads * 128 * 2};
+        uint32_t box[4] = {KC, (uint32_t)ctx->group, (uint32_t)(TILE / ctx->group), 1};
+        if (!lorc_make_tmap_bf16(&mapQ, q, 4, dims, str, box)) return cudaErrorInvalidValue;
+    }
+    if (!prefill_kv_map(ctx, khat, batch, rows, &mapK) || !prefill_kv_map(ctx, vbuf, batch, rows, &mapV)) return cudaErrorInvalidValue;
+    FaParams fp;
+    fp.out = out; fp.seq_lens = seq_lens; fp.rope_table = ctx->rope_table; fp.status = ctx->status_dev;
+    fp.T = T; fp.H_q = d.n_q_heads; fp.G = ctx->group; fp.n_rows = max_len; fp.max_pos = d.max_pos;
+    const int qp = 2 * TILE / ctx->group;                      // query positions per CTA (two blocks of 128 rows)
+    dim3 fgrid((T + qp - 1) / qp, d.n_kv_heads, batch);
+    *launches += 1;
+    return lorc_launch_dependent(lorc_prefill_attn_kernel, fgrid, dim3(F_THREADS), sizeof(FaSmem) + 1024, st, mapQ, mapK, mapV, fp);
+}
+
 cudaError_t lorc_tc_prefill_launch(lorc_ctx* ctx, const LorcLayer& L, const CacheView& cv, const CUtensorMap& mapCK,
                                    const CUtensorMap& mapCV, const CUtensorMap* mapBKT, const CUtensorMap* mapBVT,
                                    const bf16* q, bf16* out, int T, void* scratch, cudaStream_t st, int* launches) {
@@ -702,19 +731,8 @@ cudaError_t lorc_tc_prefill_launch(lorc_ctx* ctx, const LorcLayer& L, const Cach
     const int tiles = (int)(rows / TILE);
     cudaError_t e;
 
-    CUtensorMap mapQ, mapK, mapV;
-    {
-        // q [b, T, H_q, 128]: box = 64 elements x G heads x 128 / G positions
-        uint64_t dims[4] = {128, (uint64_t)d.n_q_heads, (uint64_t)T, (uint64_t)cv.batch};
-        uint64_t str[3] = {128 * 2, (uint64_t)d.n_q_heads * 128 * 2, (uint64_t)T * d.n_q_heads * 128 * 2};
-        uint32_t box[4] = {KC, (uint32_t)ctx->group, (uint32_t)(TILE / ctx->group), 1};
-        if (!lorc_make_tmap_bf16(&mapQ, q, 4, dims, str, box)) return cudaErrorInvalidValue;
-        uint64_t kd[3] = {(uint64_t)ctx->n, (uint64_t)rows, (uint64_t)cv.batch};
-        uint64_t ks[2] = {(uint64_t)ctx->n * 2, (uint64_t)rows * ctx->n * 2};
-        uint32_t kb[3] = {KC, TILE, 1};
-        if (!lorc_make_tmap_bf16(&mapK, khat, 3, kd, ks, kb)) return cudaErrorInvalidValue;
-        if (!lorc_make_tmap_bf16(&mapV, vbuf, 3, kd, ks, kb)) return cudaErrorInvalidValue;
-    }
+    CUtensorMap mapK, mapV;
+    if (!prefill_kv_map(ctx, khat, cv.batch, rows, &mapK) || !prefill_kv_map(ctx, vbuf, cv.batch, rows, &mapV)) return cudaErrorInvalidValue;
 
     RecParams rp;
     rp.seq_lens = cv.seq_lens; rp.page_table = cv.page_table; rp.rope_table = ctx->rope_table; rp.status = ctx->status_dev;
@@ -732,11 +750,5 @@ cudaError_t lorc_tc_prefill_launch(lorc_ctx* ctx, const LorcLayer& L, const Cach
     *launches += 1;
     if (e != cudaSuccess) return e;
 
-    FaParams fp;
-    fp.out = out; fp.seq_lens = cv.seq_lens; fp.rope_table = ctx->rope_table; fp.status = ctx->status_dev;
-    fp.T = T; fp.H_q = d.n_q_heads; fp.G = ctx->group; fp.n_rows = (int)rows; fp.max_pos = d.max_pos;
-    const int qp = 2 * TILE / ctx->group;                      // query positions per CTA (two blocks of 128 rows)
-    dim3 fgrid((T + qp - 1) / qp, d.n_kv_heads, cv.batch);
-    *launches += 1;
-    return lorc_launch_dependent(lorc_prefill_attn_kernel, fgrid, dim3(F_THREADS), sizeof(FaSmem) + 1024, st, mapQ, mapK, mapV, fp);
+    return lorc_tc_prefill_attend(ctx, cv.seq_lens, cv.batch, rows, (int)rows, khat, vbuf, q, out, T, st, launches);
 }

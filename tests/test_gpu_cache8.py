@@ -1,0 +1,408 @@
+"""The 8-bit cache of uncompressed layers against its fp64 restatement: cache write, decode attention, prompt chunks."""
+import numpy as np
+import pytest
+
+from oracle import cache8_oracle as C8
+
+import helpers as H
+import helpers8 as H8
+
+pytestmark = pytest.mark.gpu
+
+
+def _decode(c, scale=2.0, **over):
+    import torch
+    q, qd = c.queries(scale=scale)
+    out = torch.full((c.b, c.H_q, c.d_h), 7.0, dtype=torch.bfloat16, device="cuda")
+    c.workspace()
+    c.L.lorc_decode_attn8(c.ctx, 0, c.cache(**over), qd, out)
+    return q, H.host_f64(out).reshape(c.b, 1, c.H_q, c.d_h)
+
+
+GEOMETRIES = [(4, 2, 64), (32, 8, 128), (8, 1, 128), (3, 3, 128), (21, 3, 64), (5, 5, 64), (12, 6, 128)]
+
+
+@pytest.mark.parametrize("kind", H8.KINDS)
+@pytest.mark.parametrize("heads", GEOMETRIES)
+@pytest.mark.parametrize("lens,page", [([1], 0), ([17, 1, 64, 63], 16), ([255, 256, 257, 65], 0), ([777, 16, 300], 48), ([1030, 129], 64)])
+def test_decode(kind, heads, lens, page):
+    c = H8.Case(kind, *heads, lens, page=page, seed=len(lens))
+    q, got = _decode(c)
+    H8.assert_attention(got, *c.want(q))
+    assert c.status() == 0 and c.guard_intact()
+    c.close()
+
+
+@pytest.mark.parametrize("kind", H8.KINDS)
+@pytest.mark.parametrize("style", [0, 1, 2])
+@pytest.mark.parametrize("d_h", [64, 128])
+def test_decode_rotations_and_peaked_scores(kind, style, d_h):
+    c = H8.Case(kind, 8, 2, d_h, [900, 333], page=32, style=style, theta=500000.0, seed=style)
+    for scale in (0.01, 1.0, 16.0):
+        q, got = _decode(c, scale)
+        H8.assert_attention(got, *c.want(q))
+    assert c.status() == 0
+    c.close()
+
+
+@pytest.mark.parametrize("kind", H8.KINDS)
+def test_decode_long_and_ragged(kind):
+    """Few long sequences (many parts each), and many lengths at once (parts that begin and end inside sequences)."""
+    rng = np.random.default_rng(5)
+    for lens, page in (([8000], 0), ([5000, 8, 2500, 1], 64), (list(rng.integers(1, 900, 70)), 128)):
+        c = H8.Case(kind, 8, 2, 128, lens, page=page, seed=len(lens))
+        q, got = _decode(c)
+        H8.assert_attention(got, *c.want(q))
+        assert c.status() == 0 and c.guard_intact()
+        c.close()
+
+
+@pytest.mark.parametrize("kind", H8.KINDS)
+def test_decode_scales_of_any_size(kind):
+    """Scales that are no powers of two, differ by 2^40 between blocks, or are zero."""
+    c = H8.Case(kind, 8, 2, 128, [700, 90], seed=3)
+    c.scales = np.abs(c.rng.standard_normal(c.scales.shape)) * 1e-2
+    c.scales[1] *= np.ldexp(1.0, c.rng.integers(-40, 1, c.scales[1].shape))
+    c.scales[:, :, 2] = 0.0
+    c.scales = c.scales.astype(np.float32).astype(np.float64)
+    c.upload()
+    q, got = _decode(c)
+    H8.assert_attention(got, *c.want(q))
+    c.close()
+
+
+@pytest.mark.parametrize("kind", H8.KINDS)
+@pytest.mark.parametrize("T", [1, 5])
+def test_rows_behind_the_end_are_not_read(kind, T):
+    """Whatever stands behind a sequence's end: codes of NaN, scales that are NaN or infinite."""
+    import torch
+    c = H8.Case(kind, 32, 8, 128, [77, 5, 600], page=64, seed=4)
+    q, qd = c.queries(T)
+    c.workspace(T)
+    out = torch.zeros(c.b, T, c.H_q, c.d_h, dtype=torch.bfloat16, device="cuda")
+    call = (lambda: c.L.lorc_decode_attn8(c.ctx, 0, c.cache(), qd, out)) if T == 1 else \
+        (lambda: c.L.lorc_prefill_attn8(c.ctx, 0, c.cache(), qd, out, T))
+    call()
+    want = out.clone()
+    held = np.zeros(c.codes.shape[1:3], dtype=bool)
+    for s, n in enumerate(c.lens):
+        held[c.rows_of(s, n)] = True
+    dead = torch.from_numpy(~held).cuda()
+    c.kv[:, dead] = 0x7f
+    c.sc[:, torch.from_numpy(~held.reshape(held.shape[0], -1, 16).any(-1)).cuda()] = float("nan")
+    out.zero_()
+    call()
+    assert torch.equal(out, want)
+    H8.assert_attention(H.host_f64(out), *c.want(q, T), fp16=T > 1)
+    assert c.status() == 0
+    c.close()
+
+
+def test_empty_and_overlong_sequences():
+    import torch
+    c = H8.Case("int8", 8, 2, 128, [300, 0, 40], seed=6)
+    q, got = _decode(c)
+    H8.assert_attention(got, *c.want(q))
+    assert not got[1].any() and c.status() == c.L.LORC_ERR_EMPTY and c.status() == 0
+    # a length beyond max_seq_len: reported, zeros, the others as before
+    c.lens = [300, 0, 40]
+    c.sl.copy_(torch.tensor([300, 10 ** 6, 40], dtype=torch.int32))
+    q, got = _decode(c)
+    H8.assert_attention(got, *c.want(q))
+    assert not got[1].any() and c.status() == c.L.LORC_ERR_CAPACITY
+    c.close()
+
+
+@pytest.mark.parametrize("lens", [[200, 100], [2000, 300]])
+def test_pages_outside_the_pool_are_left_out(lens):
+    import torch
+    c = H8.Case("e4m3", 8, 2, 128, lens, page=32, seed=7)
+    q, qd = c.queries()
+    c.table[0, 2] = -1
+    c.table[1, 1] = 10 ** 6
+    c.workspace()
+    out = torch.zeros(c.b, c.H_q, c.d_h, dtype=torch.bfloat16, device="cuda")
+    c.L.lorc_decode_attn8(c.ctx, 0, c.cache(), qd, out)
+    assert c.status() == c.L.LORC_ERR_CAPACITY
+    got = H.host_f64(out)
+    for s, gone in ((0, 2), (1, 1)):
+        keep = np.arange(c.lens[s]) // 32 != gone
+        k, v = c.held(0, s, c.lens[s])[keep], c.held(1, s, c.lens[s])[keep]
+        want, size = C8.attention(k, v, c.rotate(q[s, 0], c.lens[s] - 1), c.G)
+        H8.assert_attention(got[s], want, size[:, None], np.repeat(np.abs(v).max(axis=(0, 2)), c.G)[:, None])
+    c.close()
+
+
+@pytest.mark.parametrize("kind", H8.KINDS)
+@pytest.mark.parametrize("heads,fp16", [((32, 8, 128), True), ((64, 8, 128), True), ((4, 2, 64), False), ((6, 2, 128), False)])
+@pytest.mark.parametrize("T,lens,page", [(2, [2, 40], 0), (31, [31, 64, 200], 16), (130, [130, 517], 64)])
+def test_prompt_chunks(kind, heads, fp16, T, lens, page):
+    import torch
+    c = H8.Case(kind, *heads, lens, page=page, seed=T)
+    q, qd = c.queries(T, scale=1.0)
+    out = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device="cuda")
+    c.workspace(T)
+    c.L.lorc_prefill_attn8(c.ctx, 0, c.cache(), qd, out, T)
+    H8.assert_attention(H.host_f64(out), *c.want(q, T), fp16=fp16)
+    assert c.status() == 0 and c.guard_intact()
+    c.close()
+
+
+@pytest.mark.parametrize("heads", [(32, 8, 128), (4, 2, 64)])
+def test_a_chunk_longer_than_a_sequence(heads):
+    import torch
+    c = H8.Case("int8", *heads, [50, 7, 0], seed=8)
+    q, qd = c.queries(20, scale=1.0)
+    out = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device="cuda")
+    c.workspace(20)
+    c.L.lorc_prefill_attn8(c.ctx, 0, c.cache(), qd, out, 20)
+    H8.assert_attention(H.host_f64(out), *c.want(q, 20), fp16=heads[2] == 128)
+    assert not out[1:].any() and c.status() in (c.L.LORC_ERR_ARG, c.L.LORC_ERR_EMPTY)
+    c.close()
+
+
+# ---- the write --------------------------------------------------------------------------------------------------------------
+
+def _exact_x(c, T):
+    """Hidden states with a single one each: the projections are rows of the weights, without rounding."""
+    import torch
+    at = c.rng.integers(0, c.D, (c.b, T))
+    x = np.zeros((c.b, T, c.D))
+    x[np.arange(c.b)[:, None], np.arange(T), at] = 1.0
+    return at, H.dev_bf16(x)
+
+
+@pytest.mark.parametrize("kind", H8.KINDS)
+@pytest.mark.parametrize("heads,D", [((4, 2, 64), 256), ((4, 4, 128), 512), ((3, 3, 64), 200)])
+@pytest.mark.parametrize("T,lens,page", [(1, [1, 16, 17, 32, 100], 0), (1, [49, 64, 65], 16), (15, [15, 31, 47, 40], 48),
+                                         (16, [16, 33], 0), (37, [37, 100, 64], 64), (300, [300, 333], 128)])
+def test_write_is_exact_where_the_projection_is(kind, heads, D, T, lens, page):
+    """No rotation and one-hot hidden states: codes and scales are the oracle's, bit for bit; all else stays as it was."""
+    c = H8.Case(kind, *heads, lens, page=page, D=D, style=H.ROPE_NONE, seed=T)
+    # weights of very different sizes, so that scales grow
+    for i in range(2):
+        c.w[i] = H.synth.to_bf16_exact(c.w[i] * np.ldexp(1.0, c.rng.integers(-6, 3, (D, 1))))
+    c.L.lorc_load_factors(c.ctx, 0, c.L.LORC_MODE_FULL, 0, 0, H.dev_bf16(c.w[0]), None, H.dev_bf16(c.w[1]), None)
+    at, x = _exact_x(c, T)
+    want_codes, want_scales = c.codes.copy(), c.scales.copy()
+    for s, n in enumerate(c.lens):
+        page_i, row = c.rows_of(s, -(-n // 16) * 16)
+        for i in range(2):
+            codes = want_codes[i][page_i, row].reshape(-1, c.H_kv, c.d_h)
+            scales = want_scales[i][page_i[::16], row[::16] // 16]
+            C8.write(codes, scales, np.asarray(c.w[i], dtype=np.float64)[at[s]].reshape(T, c.H_kv, c.d_h), n, kind)
+            want_codes[i][page_i, row] = codes.reshape(-1, c.n)
+            want_scales[i][page_i[::16], row[::16] // 16] = scales
+    c.workspace(T)
+    for _ in range(2):                       # the same tokens again change nothing
+        c.L.lorc_append8(c.ctx, 0, c.cache(), x, T)
+        assert np.array_equal(c.sc.double().cpu().numpy(), want_scales)
+        assert np.array_equal(H8.host_codes(c.kv, kind), want_codes)
+    assert c.status() == 0 and c.guard_intact()
+    c.close()
+
+
+@pytest.mark.parametrize("kind", H8.KINDS)
+@pytest.mark.parametrize("style", [0, 1])
+@pytest.mark.parametrize("heads,D,T,lens", [((4, 2, 64), 256, 3, [3, 50]), ((8, 8, 128), 1024, 1, [100, 31, 16]),
+                                            ((8, 2, 128), 512, 70, [70, 171]), ((2, 2, 64), 264, 9, [30]),
+                                            ((32, 8, 128), 1024, 300, [300, 417, 355])])
+def test_write_of_gaussian_tokens(kind, style, heads, D, T, lens):
+    """Every new number within half a code step of the fp64 projection (and the fp32 error of the projection)."""
+    c = H8.Case(kind, *heads, lens, page=32, D=D, style=style, theta=500000.0, seed=T + style)
+    x = H.synth.to_bf16_exact(c.rng.standard_normal((c.b, T, D)))
+    c.workspace(T)
+    c.L.lorc_append8(c.ctx, 0, c.cache(), H.dev_bf16(x), T)
+    assert c.status() == 0 and c.guard_intact()
+    c.codes, c.scales = H8.host_codes(c.kv, kind), c.sc.double().cpu().numpy()
+    x = x.astype(np.float64)
+    for s, n in enumerate(c.lens):
+        for i in range(2):
+            w = np.asarray(c.w[i], dtype=np.float64)
+            new = (x[s] @ w).reshape(T, c.H_kv, c.d_h)
+            # fp32 sums of D products: 2^-16 of the sum of magnitudes; a rotation mixes two numbers and adds 2^-22 of them
+            slack = 2.0 ** -16 * (np.abs(x[s]) @ np.abs(w)).reshape(T, c.H_kv, c.d_h)
+            if i == 0:
+                new = np.stack([c.rotate(new[t], n - T + t) for t in range(T)])
+                slack = 2 * slack.max(axis=-1, keepdims=True)
+            got = c.held(i, s, n)[n - T:]
+            page, row = c.rows_of(s, n)
+            scale = c.scales[i][page, row // 16][n - T:][..., None]
+            half = scale / 2 if kind == "int8" else np.maximum(2.0 ** -4 * np.abs(new), scale * 2.0 ** -10)
+            assert (np.abs(got - new) - (half + slack * (1 if kind == "int8" else 1.1)) <= 0).all()
+            # the scale is the smallest that holds the block's new numbers (to the projection's error), where all are new
+            for b0 in range(-(-(n - T) // 16) * 16, n, 16):
+                blk = slice(b0 - (n - T), min(n, b0 + 16) - (n - T))
+                most, off = np.abs(new[blk]).max(axis=(0, 2)), slack[blk].max()
+                sc = scale[blk][0, :, 0]
+                assert ((sc >= C8.scale_for(most - off, kind)) & (sc <= C8.scale_for(most + off, kind))).all()
+    c.close()
+
+
+@pytest.mark.parametrize("kind", H8.KINDS)
+def test_numbers_that_are_not_finite(kind):
+    """They are reported and contained: NaN becomes 0, an infinity the largest code, other heads and blocks are as ever."""
+    import torch
+    c = H8.Case(kind, 4, 2, 64, [40], D=256, style=H.ROPE_NONE, seed=9)
+    w = np.asarray(c.w[1]).copy()
+    w[7, 3], w[7, 5] = np.inf, np.nan
+    c.L.lorc_load_factors(c.ctx, 0, c.L.LORC_MODE_FULL, 0, 0, H.dev_bf16(c.w[0]), None, H.dev_bf16(w), None)
+    x = torch.zeros(1, 2, 256, dtype=torch.bfloat16, device="cuda")
+    x[0, 0, 7] = x[0, 1, 7] = 1.0
+    # 0 x inf is NaN in every row that meets them; rows of the other weights are finite
+    c.workspace(2)
+    c.L.lorc_append8(c.ctx, 0, c.cache(), x, 2)
+    assert c.status() == c.L.LORC_ERR_ARG
+    got = H8.host_codes(c.kv, kind)
+    top = C8.LARGEST[kind]
+    assert (got[1, 0, 38:40, 3] == top).all() and (got[1, 0, 38:40, 5] == 0).all()
+    assert np.isfinite(got).all() and bool(torch.isfinite(c.sc).all())
+    c.close()
+
+
+def test_write_beyond_the_capacity_and_into_bad_pages():
+    import torch
+    c = H8.Case("int8", 4, 2, 64, [20, 30, 40, 1], page=16, D=256, seed=10, max_len=48)
+    before, sc = c.kv.clone(), c.sc.clone()
+    x = torch.ones(4, 2, 256, dtype=torch.bfloat16, device="cuda")
+    c.workspace(2)
+    c.sl.copy_(torch.tensor([49, -3, 40, 1], dtype=torch.int32))
+    c.table[2, 2] = 10 ** 6
+    c.L.lorc_append8(c.ctx, 0, c.cache(), x, 2)
+    assert c.status() == c.L.LORC_ERR_CAPACITY
+    # sequence 3 has one token only: its second new token is written, nothing else changes
+    page = int(c.table[3, 0])
+    changed = (c.kv != before).any(-1)
+    assert bool(changed[:, page, 0].all())
+    changed[:, page, 0] = False
+    assert not bool(changed.any())
+    sc[:, page, 0] = c.sc[:, page, 0]
+    assert torch.equal(sc, c.sc)
+    c.close()
+
+
+@pytest.mark.parametrize("kind", H8.KINDS)
+@pytest.mark.parametrize("heads", [(32, 8, 128), (4, 2, 64)])
+def test_a_prompt_and_steps_together(kind, heads):
+    """As a program uses them: a prompt in two chunks, then steps, write and attention each time; the attention is that of the
+    numbers that the cache holds then, and these stay within their steps of the fp64 keys and values."""
+    import torch
+    D = 256
+    c = H8.Case(kind, *heads, [60, 60], page=16, D=D, seed=11, max_len=80)
+    x = H.synth.to_bf16_exact(c.rng.standard_normal((2, 70, D)))
+    xd = H.dev_bf16(x)
+    done = 0
+    for T in (33, 27, 1, 1, 1, 1, 1):
+        done += T
+        c.lens = [done, done]
+        c.sl.fill_(done)
+        c.workspace(T)
+        cache = c.cache()
+        c.L.lorc_append8(c.ctx, 0, cache, xd[:, done - T:done].contiguous(), T)
+        q, qd = c.queries(T, scale=1.0)
+        out = torch.zeros(2, T, c.H_q, c.d_h, dtype=torch.bfloat16, device="cuda")
+        if T == 1:
+            c.L.lorc_decode_attn8(c.ctx, 0, cache, qd, out)
+        else:
+            c.L.lorc_prefill_attn8(c.ctx, 0, cache, qd, out, T)
+        c.codes, c.scales = H8.host_codes(c.kv, kind), c.sc.double().cpu().numpy()
+        H8.assert_attention(H.host_f64(out), *c.want(q, T), fp16=T > 1 and heads[2] == 128)
+    assert c.status() == 0
+    for s in range(2):
+        for i in range(2):
+            new = (x[s, :done].astype(np.float64) @ np.asarray(c.w[i], dtype=np.float64)).reshape(done, c.H_kv, c.d_h)
+            if i == 0:
+                new = np.stack([c.rotate(new[t], t) for t in range(done)])
+            got = c.held(i, s, done)
+            page, row = c.rows_of(s, done)
+            scale = c.scales[i][page, row // 16][..., None]
+            # int8: half a step when written, half a step of the new scale for each time that it doubled: less than one step of the
+            # final scale in all.  e4m3: exact but for subnormals
+            half = scale if kind == "int8" else 2.0 ** -4 * np.abs(new) + scale * 2.0 ** -9
+            assert (np.abs(got - new) <= half + 2.0 ** -12).all()
+    c.close()
+
+
+def test_other_streams_and_a_captured_graph():
+    import torch
+    c = H8.Case("int8", 8, 2, 128, [400, 900], page=64, D=256, seed=12, max_len=960)
+    c.workspace(1)
+    x = H.dev_bf16(c.rng.standard_normal((2, 1, 256)))
+    q, qd = c.queries()
+    out = torch.zeros(2, 8, 128, dtype=torch.bfloat16, device="cuda")
+    cache = c.cache()
+
+    def step():
+        c.L.lorc_append8(c.ctx, 0, cache, x)
+        c.L.lorc_decode_attn8(c.ctx, 0, cache, qd, out)
+
+    step()
+    torch.cuda.synchronize()
+    want, kv = out.clone(), c.kv.clone()
+    out.zero_()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step()
+    side.synchronize()
+    assert torch.equal(out, want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step()
+    for length in ([400, 900], [401, 77]):
+        c.sl.copy_(torch.tensor(length, dtype=torch.int32))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        step()
+        torch.cuda.synchronize()
+        assert torch.equal(out, got)
+        if length == [400, 900]:
+            assert torch.equal(got, want) and torch.equal(c.kv, kv)
+    assert c.status() == 0
+    c.close()
+
+
+def test_refusals():
+    import torch
+    L = H.lib()
+    c = H8.Case("int8", 8, 2, 128, [40], page=16, D=256, seed=13)
+    c.workspace(4)
+    q = torch.zeros(1, 8, 128, dtype=torch.bfloat16, device="cuda")
+    x = torch.zeros(1, 4, 256, dtype=torch.bfloat16, device="cuda")
+    out = torch.zeros_like(q)
+
+    def refused(code, call, *a, **k):
+        with pytest.raises(L.LorcError) as e:
+            call(*a, **k)
+        assert e.value.code == code, str(e.value)
+
+    for bad in (dict(k=None), dict(v_scale=None), dict(seq_lens=None), dict(batch=0), dict(max_seq_len=0), dict(max_seq_len=81),
+                dict(type=2), dict(page_size=8), dict(page_size=0), dict(max_pages_per_seq=1), dict(n_pages=0),
+                dict(k=c.kv.data_ptr() + 8), dict(k_scale=c.sc.data_ptr() + 2), dict(page_table=None, seq_stride=40),
+                dict(page_table=None, seq_stride=0)):
+        refused(L.LORC_ERR_ARG, L.lorc_decode_attn8, c.ctx, 0, c.cache(**bad), q, out)
+        refused(L.LORC_ERR_ARG, L.lorc_append8, c.ctx, 0, c.cache(**bad), x, 1)
+        refused(L.LORC_ERR_ARG, L.lorc_prefill_attn8, c.ctx, 0, c.cache(**bad), q, out, 1)
+    refused(L.LORC_ERR_ARG, L.lorc_decode_attn8, c.ctx, 0, c.cache(), None, out)
+    refused(L.LORC_ERR_ARG, L.lorc_decode_attn8, c.ctx, 0, c.cache(), q, None)
+    refused(L.LORC_ERR_ARG, L.lorc_decode_attn8, c.ctx, 0, c.cache(), q.data_ptr() + 2, out)
+    refused(L.LORC_ERR_LAYER, L.lorc_decode_attn8, c.ctx, 1, c.cache(), q, out)
+    for T in (0, -1, 41):
+        refused(L.LORC_ERR_ARG, L.lorc_append8, c.ctx, 0, c.cache(), x, T)
+        refused(L.LORC_ERR_ARG, L.lorc_prefill_attn8, c.ctx, 0, c.cache(), q, out, T)
+    L.lorc_set_workspace(c.ctx, None)
+    refused(L.LORC_ERR_WORKSPACE, L.lorc_decode_attn8, c.ctx, 0, c.cache(), q, out)
+    refused(L.LORC_ERR_WORKSPACE, L.lorc_append8, c.ctx, 0, c.cache(), x, 4)
+    L.lorc_set_workspace(c.ctx, c.ws, 256)
+    refused(L.LORC_ERR_WORKSPACE, L.lorc_append8, c.ctx, 0, c.cache(), x, 4)
+    assert L.lorc_cache8_workspace_bytes(c.ctx, 0, 40, 1) == 0 and L.lorc_cache8_workspace_bytes(c.ctx, 1, 40, 0) == 0
+    # a compressed layer
+    ctx = L.lorc_create(2, 256, 8, 2, 128, 10000.0, max_pos=64)
+    a, f = torch.zeros(256, 32, dtype=torch.bfloat16, device="cuda"), torch.zeros(32, 256, dtype=torch.bfloat16, device="cuda")
+    L.lorc_load_factors(ctx, 0, L.LORC_MODE_LATENT, 32, 32, a, f, a, f)
+    L.lorc_set_workspace(ctx, c.ws)
+    refused(L.LORC_ERR_UNSUPPORTED, L.lorc_decode_attn8, ctx, 0, c.cache(), q, out)
+    refused(L.LORC_ERR_LAYER, L.lorc_decode_attn8, ctx, 1, c.cache(), q, out)
+    L.lorc_destroy(ctx)
+    assert c.status() == 0
+    c.close()
