@@ -27,8 +27,9 @@ using namespace sm100;
 
 namespace {
 
-constexpr int D8_TILE = 64;          // tokens per stage (16 per consumer warp)
-constexpr int D8_STAGES = 5;
+constexpr int D8_TILE = 128;         // tokens per stage (32 per consumer warp)
+constexpr int D8_UNIT = 64;          // tokens by which work is dealt out
+constexpr int D8_STAGES = 3;
 constexpr int D8_THREADS = 160;      // warps 0..3 consumers, warp 4 TMA
 constexpr int D8_BLOCKS_PER_SM = 2;
 constexpr float D8_RAISE = 8.f;
@@ -74,7 +75,7 @@ __device__ __forceinline__ float ex2_approx(float x) {
 template <int DH>
 struct D8Smem {
     uint8_t kv[D8_STAGES][2][D8_TILE * DH];     // keys, values of a stage: rows of DH bytes, swizzled (128 or 64 bytes)
-    float o[4][8][DH + 4];                      // at the end of a sequence's part: every warp's un-normalised output
+    float o[4][4][DH + 4];                      // at the end of a sequence's part: every warp's un-normalised output, four heads at a time
     float qs[8][DH];                            // rotated queries of the G heads (rows G..7 zero)
     float m[4][8], l[4][8], vs[4];
     uint64_t full[D8_STAGES], empty[D8_STAGES];
@@ -104,8 +105,8 @@ __device__ __forceinline__ int d8_len(const D8Params& p, int r, int* status) {
     }
     return len - (p.T - 1 - (r - s * p.T));
 }
-// Steps of a row on the list; a row without tokens has one, in which its zeros are written.
-__device__ __forceinline__ int d8_weight(int len) { return len <= 0 ? 1 : (len - 1) / D8_TILE + 1; }
+// Units of a row on the list; a row without tokens has one, in which its zeros are written.
+__device__ __forceinline__ int d8_weight(int len) { return len <= 0 ? 1 : (len - 1) / D8_UNIT + 1; }
 
 // Sum of the weights of rows [0, n); whole warps.
 __device__ __forceinline__ long long d8_total(const D8Params& p, int n, int lane) {
@@ -191,11 +192,13 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
     const D8Range range = d8_range(p, part, lane);
     __syncthreads();                             // the barriers are initialised
     bool ok = true;
-    int step = 0;                                // steps of the stage ring so far
+    int st = 0;                                  // place in the ring of stages
+    uint32_t par = 0;                            // and the parity of this round
 
     if (warp == 4) {
         // ------------------------------------------------------------------ producer (one elected lane issues)
-        const int nbox = D8_TILE / p.box_rows;   // boxes per tile: 1, or up to 4 on small pages
+        const int nbox = D8_TILE / p.box_rows;   // boxes per tile: 2, or up to 8 on small pages
+        int fetched = 0;                         // stages that may have copies under way
         long long f = range.f, first = range.first;
         for (int row = range.row; f < range.end && ok; ++row) {
             const int s = row / p.T, len = d8_len(p, row, nullptr), w = d8_weight(len);
@@ -217,24 +220,26 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
                 }
                 return page;
             };
-            int t0 = (int)(f - first) * D8_TILE;
+            int t0 = (int)(f - first) * D8_UNIT;
+            const int t_end = min(len, (int)(stop - first) * D8_UNIT);
             int mine = lookup(t0);
-            for (; f < stop; ++f, t0 += D8_TILE, ++step) {
-                const int st = step % D8_STAGES;
-                int pages[4];
+            for (; t0 < t_end; t0 += D8_TILE) {
+                int pages[8];
                 const uint32_t dead = __ballot_sync(0xffffffffu, mine < 0);
                 if (mine < 0) mine = cv.n_pages;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) pages[j] = __shfl_sync(0xffffffffu, mine, j);
-                if (f + 1 < stop) mine = lookup(t0 + D8_TILE);
-                ok = __all_sync(0xffffffffu, mbar_wait(&sm.empty[st], ((step / D8_STAGES) & 1) ^ 1));
+                for (int j = 0; j < 8; ++j) pages[j] = __shfl_sync(0xffffffffu, mine, j);
+                if (t0 + D8_TILE < t_end) mine = lookup(t0 + D8_TILE);
+                ok = __all_sync(0xffffffffu, mbar_wait(&sm.empty[st], par ^ 1));
                 if (!ok) break;
                 if (elect_one()) {
+                    // boxes wholly behind the part's end are not fetched
+                    const int live = min(nbox, (t_end - t0 + p.box_rows - 1) / p.box_rows);
                     sm.dead[st] = dead;
-                    mbar_arrive_expect_tx(&sm.full[st], 2 * D8_TILE * DH);
+                    mbar_arrive_expect_tx(&sm.full[st], 2 * DH * p.box_rows * live);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        if (j >= nbox) break;
+                    for (int j = 0; j < 8; ++j) {
+                        if (j >= live) break;
                         const int tok = t0 + j * p.box_rows;
                         const int y = cv.page_table ? tok % cv.page_size : tok, z = cv.page_table ? pages[j] : s;
                         tma_load_3d(sm.kv[st][0] + j * p.box_rows * DH, &mapK, &sm.full[st], kvh * DH, y, z);
@@ -242,12 +247,17 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
                     }
                 }
                 __syncwarp();
+                if (++st == D8_STAGES) { st = 0; par ^= 1; }
+                if (fetched < D8_STAGES) ++fetched;
             }
+            f = stop;
             first += w;
         }
         // The block stays until the copies into its shared memory have landed, also when a wait has run out.
-        for (int j = max(step - D8_STAGES, 0); j < step; ++j)
-            if (!mbar_wait(&sm.full[j % D8_STAGES], (j / D8_STAGES) & 1)) ok = false;
+        for (; fetched > 0; --fetched) {
+            if (--st < 0) { st = D8_STAGES - 1; par ^= 1; }
+            if (!mbar_wait(&sm.full[st], par)) ok = false;
+        }
         if (!ok && lane == 0) lorc_set_status(p.status, LORC_ERR_TIMEOUT);
         return;
     }
@@ -256,22 +266,21 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
     // byte offset of this lane's row in a stage and the row's swizzle; ldmatrix.x4 takes four 8 x 8 matrices of words, lane
     // mi = lane / 8 addresses a row of matrix mi: (tokens 0..7 | 8..15) x piece, then the same x the next piece
     const int mi = lane >> 3, lr = lane & 7;
-    const uint32_t my_row = (uint32_t)(warp * 16 + (mi & 1) * 8 + lr);
+    const uint32_t my_row = (uint32_t)(warp * 32 + (mi & 1) * 8 + lr);
     const uint32_t row_off = my_row * DH, sw = DH == 128 ? my_row & 7 : (my_row >> 1) & 3;
-    const int box = warp * 16 / p.box_rows;      // the box of a stage that holds this warp's tokens
+    const int box0 = warp * 32 / p.box_rows, box1 = (warp * 32 + 16) / p.box_rows;      // the boxes of this warp's tokens
     long long f = range.f, first = range.first;
     for (int row = range.row; f < range.end; ++row) {
         const int s = row / p.T, len = d8_len(p, row, tid == 0 ? p.status : nullptr), w = d8_weight(len);
         const long long stop = first + w < range.end ? first + w : range.end;
         const bool whole = f == first && stop == first + w;
-        const int n_steps = len > 0 ? (int)(stop - f) : 0;
-        const int t_begin = (int)(f - first) * D8_TILE, t_end = min(len, (int)(stop - first) * D8_TILE);
+        const int t_begin = (int)(f - first) * D8_UNIT, t_end = min(len, (int)(stop - first) * D8_UNIT);
 
-        // the scales of this warp's blocks, 32 steps at a time: lane j holds those of step j
-        auto scales = [&](int i0, float& ks, float& vs) {
-            const int pos = t_begin + (i0 + lane) * D8_TILE + warp * 16;
+        // the scales of this warp's blocks, two a step, 16 steps at a time: lane 2 j + u holds block u of step j
+        auto scales = [&](int t0, float& ks, float& vs) {
+            const int pos = t0 + (lane >> 1) * D8_TILE + warp * 32 + (lane & 1) * 16;
             ks = vs = 0.f;
-            if (i0 + lane < n_steps && pos < t_end) {
+            if (pos < t_end) {
                 const long long at = lorc_block8(cv, s, pos / LORC_BLOCK8);
                 if (at >= 0) {
                     ks = cv.k_scale[at * p.n_kv + kvh];
@@ -280,7 +289,7 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
             }
         };
         float ks_now, vs_now, ks_next = 0.f, vs_next = 0.f;
-        scales(0, ks_now, vs_now);
+        scales(t_begin, ks_now, vs_now);
 
         // RoPE(q, position) for the G heads of this KV head
         for (int i = tid; i < 8 * (DH / 2); i += 128) {
@@ -333,53 +342,70 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
         float m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};   // heads 2 t, 2 t + 1 (l: this lane's tokens)
         float v_ref = 0.f, v_inv = 0.f;          // largest scale of values so far: o is in units of it
 
-        for (int i = 0; i < n_steps; ++i, ++step) {
-            const int st = step % D8_STAGES, tw = t_begin + i * D8_TILE + warp * 16;     // first token of this warp
-            if (!ok) continue;
-            if ((i & 31) == 0) {
-                if (i > 0) { ks_now = ks_next; vs_now = vs_next; }
-                if (i + 32 < n_steps) scales(i + 32, ks_next, vs_next);
+        int turn = 0;
+        for (int t0 = t_begin; t0 < t_end && ok; t0 += D8_TILE, turn = (turn + 2) & 31) {
+            const int tw = t0 + warp * 32;       // first token of this warp
+            if (turn == 0) {
+                if (t0 > t_begin) { ks_now = ks_next; vs_now = vs_next; }
+                if (t0 + 16 * D8_TILE < t_end) scales(t0 + 16 * D8_TILE, ks_next, vs_next);
             }
-            const float k_scale = __shfl_sync(0xffffffffu, ks_now, i & 31), v_scale = __shfl_sync(0xffffffffu, vs_now, i & 31);
-            ok = __all_sync(0xffffffffu, mbar_wait(&sm.full[st], (step / D8_STAGES) & 1));
-            if (!ok) continue;
-            const int t_live = (sm.dead[st] >> box) & 1 ? 0 : t_end;
+            float k_scale[2], v_scale[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                k_scale[u] = __shfl_sync(0xffffffffu, ks_now, turn + u);
+                v_scale[u] = __shfl_sync(0xffffffffu, vs_now, turn + u);
+            }
+            ok = __all_sync(0xffffffffu, mbar_wait(&sm.full[st], par));
+            if (!ok) break;
             const uint32_t k0 = smem_u32(sm.kv[st][0]) + row_off, v0 = smem_u32(sm.kv[st][1]) + row_off;
-            // scores of tokens g, g + 8 against heads 2 t, 2 t + 1; four short chains
-            float sc[4][4];
+            // scores of tokens g, g + 8 of both blocks against heads 2 t, 2 t + 1
+            float x[2][4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) sc[j][0] = sc[j][1] = sc[j][2] = sc[j][3] = 0.f;
+            for (int u = 0; u < 2; ++u) {
+                float sc[2][4];
 #pragma unroll
-            for (int k2 = 0; k2 < KS / 2; ++k2) {
-                uint32_t a[4];
-                ldmatrix_x4(a, k0 + (((2 * k2 + (mi >> 1)) ^ sw) << 4));
+                for (int j = 0; j < 2; ++j) sc[j][0] = sc[j][1] = sc[j][2] = sc[j][3] = 0.f;
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    uint32_t a0, a1, a2, a3;
-                    lorc_codes_half<E4M3, 0, 1, 2, 3>(a[2 * e], a0, a2);
-                    lorc_codes_half<E4M3, 0, 1, 2, 3>(a[2 * e + 1], a1, a3);
-                    mma_f16_16816(sc[e], a0, a1, a2, a3, qhi[2 * k2 + e][0], qhi[2 * k2 + e][1]);
-                    mma_f16_16816(sc[2 + e], a0, a1, a2, a3, qlo[2 * k2 + e][0], qlo[2 * k2 + e][1]);
+                for (int k2 = 0; k2 < KS / 2; ++k2) {
+                    uint32_t a[4];
+                    ldmatrix_x4(a, k0 + u * 16 * DH + (((2 * k2 + (mi >> 1)) ^ sw) << 4));
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        uint32_t a0, a1, a2, a3;
+                        lorc_codes_half<E4M3, 0, 1, 2, 3>(a[2 * e], a0, a2);
+                        lorc_codes_half<E4M3, 0, 1, 2, 3>(a[2 * e + 1], a1, a3);
+                        mma_f16_16816(sc[0], a0, a1, a2, a3, qhi[2 * k2 + e][0], qhi[2 * k2 + e][1]);
+                        mma_f16_16816(sc[1], a0, a1, a2, a3, qlo[2 * k2 + e][0], qlo[2 * k2 + e][1]);
+                    }
+                }
+                const float f0 = factor[0] * k_scale[u], f1 = factor[1] * k_scale[u];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[u][j] = (sc[0][j] + sc[1][j]) * (j & 1 ? f1 : f0);
+            }
+            const uint32_t dead = sm.dead[st];
+            if (tw + 32 > t_end || dead) {       // tokens past the end, or in pages that do not exist
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int live = (dead >> (u ? box1 : box0)) & 1 ? 0 : t_end - tw - 16 * u;
+                    if (live <= 0) v_scale[u] = 0.f;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (g + (j >> 1) * 8 >= live) x[u][j] = -INFINITY;
+                }
+                if (E4M3) {
+                    // such rows have the factor zero, but their bytes may be codes of NaN
+                    for (int r = max(t_end - tw, 0); r < 32; ++r)
+                        if (lane < DH / 8) *reinterpret_cast<uint2*>(sm.kv[st][1] + (warp * 32 + r) * DH + lane * 8) = make_uint2(0u, 0u);
+                    fence_proxy_async_smem();    // before the stage's next copy
+                    __syncwarp();
                 }
             }
-            float x[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                x[j] = ((sc[0][j] + sc[1][j]) + (sc[2][j] + sc[3][j])) * (factor[j & 1] * k_scale);
-                if (tw + g + (j >> 1) * 8 >= t_live) x[j] = -INFINITY;
-            }
-            // running softmax over this warp's tokens
-            float mx[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                mx[e] = fmaxf(x[e], x[2 + e]);
-#pragma unroll
-                for (int d = 4; d < 32; d <<= 1) mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], d));
-            }
-            const float v_mag = tw < t_live ? fabsf(v_scale) : 0.f;
-            const bool raise0 = mx[0] > m_run[0] + D8_RAISE;
-            const bool raise1 = mx[1] > m_run[1] + D8_RAISE;
-            if (__any_sync(0xffffffffu, raise0 || raise1 || v_mag > v_ref)) {
+            // running softmax over this warp's tokens: the reference is raised when a score exceeds it by more than 2^8, which
+            // after the first steps is rare, so the maximum is looked for only then
+            const float top0 = fmaxf(fmaxf(x[0][0], x[0][2]), fmaxf(x[1][0], x[1][2]));
+            const float top1 = fmaxf(fmaxf(x[0][1], x[0][3]), fmaxf(x[1][1], x[1][3]));
+            const float v_mag = fmaxf(fabsf(v_scale[0]), fabsf(v_scale[1]));
+            if (__any_sync(0xffffffffu, top0 > m_run[0] + D8_RAISE || top1 > m_run[1] + D8_RAISE || v_mag > v_ref)) {
                 float shrink = 1.f;
                 if (v_mag > v_ref) {
                     const float now = fmaxf(v_mag, 1e-35f);
@@ -389,10 +415,13 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
                 }
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
+                    float mx = e ? top1 : top0;
+#pragma unroll
+                    for (int d = 4; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
                     float alpha = 1.f;
-                    if (e ? raise1 : raise0) {
-                        alpha = m_run[e] == -INFINITY ? 0.f : ex2_approx(m_run[e] - mx[e]);
-                        m_run[e] = mx[e];
+                    if (mx > m_run[e] + D8_RAISE) {
+                        alpha = m_run[e] == -INFINITY ? 0.f : ex2_approx(m_run[e] - mx);
+                        m_run[e] = mx;
                     }
                     l_run[e] *= alpha;
                     alpha *= shrink;
@@ -403,51 +432,39 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
                     }
                 }
             }
-            // p = 2^(x - m); c p in two fp16 parts, pairs of heads
-            const float c = tw < t_live ? v_scale * v_inv : 0.f;
-            uint32_t ph[2], pl[2];
+            // p = 2^(x - m); c p as fp16, pairs of heads
+            const float m0 = m_run[0] == -INFINITY ? 0.f : m_run[0], m1 = m_run[1] == -INFINITY ? 0.f : m_run[1];
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                float e2[2];
+            for (int u = 0; u < 2; ++u) {
+                const float c = v_scale[u] * v_inv;
+                uint32_t ph[2];
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const float m = m_run[e] == -INFINITY ? 0.f : m_run[e];          // nothing seen yet: 2^(-inf) = 0
-                    const float pr = ex2_approx(x[2 * j + e] - m);
-                    l_run[e] += pr;
-                    e2[e] = pr * c;
+                for (int j = 0; j < 2; ++j) {
+                    const float p0 = ex2_approx(x[u][2 * j] - m0), p1 = ex2_approx(x[u][2 * j + 1] - m1);
+                    l_run[0] += p0;
+                    l_run[1] += p1;
+                    ph[j] = pack_half(p0 * c, p1 * c);
                 }
-                ph[j] = pack_half(e2[0], e2[1]);
-                const float2 back = unpack_half(ph[j]);
-                pl[j] = pack_half(e2[0] - back.x, e2[1] - back.y);
-            }
-            const uint32_t b0 = movmatrix_trans(ph[0]), b1 = movmatrix_trans(ph[1]);
-            const uint32_t c0 = movmatrix_trans(pl[0]), c1 = movmatrix_trans(pl[1]);
-            if (E4M3 && tw + 16 > t_end) {
-                // rows past the end have the factor zero; their bytes may be codes of NaN
-                for (int r = max(t_end - tw, 0); r < 16; ++r)
-                    if (lane < DH / 8) *reinterpret_cast<uint2*>(sm.kv[st][1] + (warp * 16 + r) * DH + lane * 8) = make_uint2(0u, 0u);
-                fence_proxy_async_smem();        // before the stage's next copy
-                __syncwarp();
-            }
-            // O^T += V^T (c P)^T
+                const uint32_t b0 = movmatrix_trans(ph[0]), b1 = movmatrix_trans(ph[1]);
+                // O^T += V^T (c P)^T
 #pragma unroll
-            for (int k2 = 0; k2 < KS / 2; ++k2) {
-                uint32_t a[4];
-                ldmatrix_x4_trans(a, v0 + (((2 * k2 + (mi >> 1)) ^ sw) << 4));
+                for (int k2 = 0; k2 < KS / 2; ++k2) {
+                    uint32_t a[4];
+                    ldmatrix_x4_trans(a, v0 + u * 16 * DH + (((2 * k2 + (mi >> 1)) ^ sw) << 4));
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    uint32_t a0, a1, a2, a3;
-                    lorc_codes_half<E4M3, 0, 2, 1, 3>(a[2 * e], a0, a1);
-                    lorc_codes_half<E4M3, 0, 2, 1, 3>(a[2 * e + 1], a2, a3);
-                    mma_f16_16816(o[2 * k2 + e], a0, a1, a2, a3, b0, b1);
-                    mma_f16_16816(o[2 * k2 + e], a0, a1, a2, a3, c0, c1);
+                    for (int e = 0; e < 2; ++e) {
+                        uint32_t a0, a1, a2, a3;
+                        lorc_codes_half<E4M3, 0, 2, 1, 3>(a[2 * e], a0, a1);
+                        lorc_codes_half<E4M3, 0, 2, 1, 3>(a[2 * e + 1], a2, a3);
+                        mma_f16_16816(o[2 * k2 + e], a0, a1, a2, a3, b0, b1);
+                    }
                 }
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(&sm.empty[st]);
+            if (++st == D8_STAGES) { st = 0; par ^= 1; }
         }
-        // what the four warps have
-        const float v_unit = v_ref;
+        // what the four warps have, four heads at a time
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
 #pragma unroll
@@ -456,36 +473,41 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
                 sm.m[warp][2 * t + e] = m_run[e];
                 sm.l[warp][2 * t + e] = l_run[e];
             }
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                sm.o[warp][2 * t + e][16 * ks + 2 * g] = o[ks][e];
-                sm.o[warp][2 * t + e][16 * ks + 2 * g + 1] = o[ks][2 + e];
-            }
         }
-        if (lane == 0) sm.vs[warp] = v_unit;
-        __syncwarp();
-        asm volatile("bar.sync 1, 128;" ::: "memory");
-        for (int i = tid; i < G * DH; i += 128) {
-            const int h = i / DH, d = i - h * DH;
-            float M = -INFINITY;
+        if (lane == 0) sm.vs[warp] = v_ref;
+        for (int h0 = 0; h0 < G; h0 += 4) {
+            if (2 * t >= h0 && 2 * t < h0 + 4)
 #pragma unroll
-            for (int x = 0; x < 4; ++x)
-                if (sm.l[x][h] != 0.f) M = fmaxf(M, sm.m[x][h]);
-            float L = 0.f, acc = 0.f;
+                for (int e = 0; e < 2; ++e)
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const float wgt = sm.l[x][h] != 0.f ? exp2f(sm.m[x][h] - M) : 0.f;
-                L += wgt * sm.l[x][h];
-                acc += wgt * sm.vs[x] * sm.o[x][h][d];
+                    for (int ks = 0; ks < KS; ++ks)
+                        *reinterpret_cast<float2*>(&sm.o[warp][2 * t + e - h0][16 * ks + 2 * g]) = make_float2(o[ks][e], o[ks][2 + e]);
+            __syncwarp();
+            asm volatile("bar.sync 1, 128;" ::: "memory");
+            const int heads = min(G - h0, 4);
+            for (int i = tid; i < heads * DH; i += 128) {
+                const int h = h0 + i / DH, d = i % DH;
+                float M = -INFINITY;
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+                    if (sm.l[x][h] != 0.f) M = fmaxf(M, sm.m[x][h]);
+                float L = 0.f, acc = 0.f;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const float wgt = sm.l[x][h] != 0.f ? exp2f(sm.m[x][h] - M) : 0.f;
+                    L += wgt * sm.l[x][h];
+                    acc += wgt * sm.vs[x] * sm.o[x][h - h0][d];
+                }
+                if (whole) {
+                    p.out[((long long)row * H_q + kvh * G + h) * DH + d] = __float2bfloat16_rn(L != 0.f ? acc / L : 0.f);
+                    if (L == 0.f && d == 0) lorc_set_status(p.status, LORC_ERR_EMPTY);
+                } else {
+                    const long long unit = ((long long)kvh * (p.parts + p.rows) + part + row) * G + h;
+                    if (d == 0) *reinterpret_cast<float2*>(p.part_ml + unit * 2) = make_float2(M, L);
+                    p.part_o[unit * DH + d] = acc;
+                }
             }
-            if (whole) {
-                p.out[((long long)row * H_q + kvh * G + h) * DH + d] = __float2bfloat16_rn(L != 0.f ? acc / L : 0.f);
-                if (L == 0.f && d == 0) lorc_set_status(p.status, LORC_ERR_EMPTY);
-            } else {
-                const long long unit = ((long long)kvh * (p.parts + p.rows) + part + row) * G + h;
-                if (d == 0) *reinterpret_cast<float2*>(p.part_ml + unit * 2) = make_float2(M, L);
-                p.part_o[unit * DH + d] = acc;
-            }
+            if (h0 + 4 < G) asm volatile("bar.sync 1, 128;" ::: "memory");
         }
         first += w;
         f = stop;
@@ -548,7 +570,7 @@ void d8_plan(const lorc_ctx* ctx, int rows, int max_seq_len, int T, int* parts, 
     const int slots = D8_BLOCKS_PER_SM * ctx->sm_count / ctx->desc.n_kv_heads;
     *parts = slots > 1 ? slots : 1;
     *least = 2;
-    if (max_seq_len <= 4 * D8_TILE || (T > 1 && rows >= *parts)) *parts = 0;
+    if (max_seq_len <= 4 * D8_UNIT || (T > 1 && rows >= *parts)) *parts = 0;
 }
 
 size_t d8_ml_bytes(const lorc_ctx* ctx, long long slots) {
@@ -577,7 +599,7 @@ size_t lorc_decode8_scratch_bytes(const lorc_ctx* ctx, int batch, int max_seq_le
     // a call may have fewer tokens or shorter sequences than stated here: room for the list in any case
     int parts, least;
     const long long rows = (long long)batch * T;
-    d8_plan(ctx, 1, max_seq_len > 4 * D8_TILE ? max_seq_len : 4 * D8_TILE + 1, 1, &parts, &least);
+    d8_plan(ctx, 1, max_seq_len > 4 * D8_UNIT ? max_seq_len : 4 * D8_UNIT + 1, 1, &parts, &least);
     const long long slots = parts + (batch > parts || rows <= batch ? batch : rows < parts ? rows : parts);
     return d8_ml_bytes(ctx, slots) + lorc_align_up((size_t)slots * ctx->desc.n_q_heads * ctx->desc.d_head * sizeof(float), 256);
 }

@@ -138,13 +138,14 @@ def assert_attention(got, want, size, vmax, fp16=False):
     """Element by element: half a step of the bf16 output, 2^-8 |want|, and the arithmetic.  With A = sum |q_i k_i| / sqrt(d):
     a score in fp32 is off by at most 128 sums of 2^-24 A and 2^-22 A for the rotation and the two fp16 parts of the query,
     together less than 2^-16.5 A; a change of every score by at most e moves a softmax average by at most 2 e max|v|
-    (up to second order); exponentials, products and sums of at most 2^13 numbers add less than 2^-15 max|v|.  So
-    2^-15 (1 + A) max|v|.  fp16 (the tcgen05 kernel rounds rotated queries and probabilities, and the expanded numbers, to fp16,
+    (up to second order); exponentials, products and sums of at most 2^13 numbers add less than 2^-15 max|v|; probabilities times
+    scale are rounded to fp16 in the numerator, half a step each, which moves the average by at most 2^-11 max|v|.  So
+    (2^-11 + 2^-15 (1 + A)) max|v|.  fp16 (the tcgen05 kernel rounds rotated queries and probabilities, and the expanded numbers, to fp16,
     half a step is 2^-11): scores are off by 2^-11 A, 2^-10 A max|v| in the average, probabilities add 2 2^-11 max|v|:
     (2^-10 + 2^-15) (1 + A) max|v|."""
     got = np.asarray(got, dtype=np.float64)
-    unit = (2.0 ** -10 + 2.0 ** -15) if fp16 else 2.0 ** -15
-    bound = 2.0 ** -8 * np.abs(want) + unit * (1 + size) * vmax
+    arithmetic = (2.0 ** -10 + 2.0 ** -15) * (1 + size) if fp16 else 2.0 ** -11 + 2.0 ** -15 * (1 + size)
+    bound = 2.0 ** -8 * np.abs(want) + arithmetic * vmax
     excess = np.abs(got - want) - bound
     assert np.isfinite(got).all()
     assert excess.max() <= 0, (float(excess.max()), np.unravel_index(excess.argmax(), excess.shape))
