@@ -126,7 +126,7 @@ typedef struct lorc_cache {
 } lorc_cache;
 
 /* Create / destroy a context.  Creation allocates only library-owned tables
- * (the cos/sin table of max_pos x d_head/2 pairs and a status word; per-layer
+ * (the cos/sin table of max_pos x d_head/2 pairs, a status word and some counters; per-layer
  * factor copies come later, in lorc_load_factors).  Uses the current CUDA device.
  * Errors: ARG (null, non-positive sizes, n_q_heads not a multiple of
  * n_kv_heads), UNSUPPORTED (d_head not 64/128, more than 8 query heads per KV

@@ -43,6 +43,7 @@ int check8(lorc_ctx* ctx, int layer, const lorc_cache8* c, int T, const void* in
     if (c->max_seq_len > capacity) return fail8(ctx, LORC_ERR_ARG, "cache8: max_seq_len exceeds the cache capacity");
     if (T <= 0 || T > c->max_seq_len) return fail8(ctx, LORC_ERR_ARG, "cache8: T must be positive and not exceed max_seq_len");
     if ((long long)c->batch * T > 0x3fffffffll) return fail8(ctx, LORC_ERR_ARG, "cache8: batch * T is too large");
+    if ((long long)c->batch * T * ((c->max_seq_len - 1) / 64 + 1) >= 1ll << 30) return fail8(ctx, LORC_ERR_ARG, "cache8: batch * T * max_seq_len is too large");
     int dev = -1;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return fail8_cuda(ctx, e, "cache8");

@@ -57,6 +57,7 @@ struct lorc_ctx {
     std::vector<LorcLayer> layers;
     float2* rope_table = nullptr;   // [max_pos][d_head/2] (cos, sin)
     int* status_dev = nullptr;
+    unsigned* part_count = nullptr; // [lorc_part_counters()] zero between calls: parts of a sequence that are done (decode8.cu)
     void* ws = nullptr;
     size_t ws_bytes = 0;
     std::string err;
@@ -68,6 +69,10 @@ struct lorc_ctx {
     LorcProfile* prof = nullptr;   // event bookkeeping, created on first use
     bool prof_on = false;          // LORC_FLAG_PROFILE or lorc_profile_enable
 };
+
+// Counters that the attention over the 8-bit cache needs: a part of the work list and KV head each, which are two blocks per SM at
+// most, or one per KV head.
+static inline size_t lorc_part_counters(int sm_count, int n_kv_heads) { return 2 * (size_t)sm_count + n_kv_heads; }
 
 // RAII bracket: records an event pair around the launches issued in its scope (no-op unless profiling).
 struct LorcStageTimer {

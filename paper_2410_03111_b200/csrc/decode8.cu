@@ -16,7 +16,8 @@
 //
 // The steps (64 tokens) of all sequences form one list, cut into equal parts for the blocks of a KV head that are resident at
 // once: all of them stream from the start to the end of the launch whatever the lengths are.  A part may begin and end inside
-// a sequence; what it computes of a sequence that it does not hold alone goes to memory, un-normalised, for a merge kernel.
+// a sequence; what it computes of a sequence that it does not hold alone goes to memory, un-normalised, and the last of the
+// sequence's parts to get there adds them up.  (A merge kernel of its own cost 6 to 8 us more.)
 #include <math.h>
 
 #include "cache8.cuh"
@@ -30,7 +31,7 @@ namespace {
 constexpr int D8_TILE = 128;         // tokens per stage (32 per consumer warp)
 constexpr int D8_UNIT = 64;          // tokens by which work is dealt out
 constexpr int D8_STAGES = 3;
-constexpr int D8_THREADS = 160;      // warps 0..3 consumers, warp 4 TMA
+constexpr int D8_THREADS = 192;      // warps 0..3 consumers, warp 4 TMA and scales, warp 5 queries
 constexpr int D8_BLOCKS_PER_SM = 2;
 constexpr float D8_RAISE = 8.f;
 constexpr float LOG2E = 1.4426950408889634f;
@@ -78,8 +79,10 @@ struct D8Smem {
     float o[4][4][DH + 4];                      // at the end of a sequence's part: every warp's un-normalised output, four heads at a time
     float qs[8][DH];                            // rotated queries of the G heads (rows G..7 zero)
     float m[4][8], l[4][8], vs[4];
-    uint64_t full[D8_STAGES], empty[D8_STAGES];
-    uint32_t dead[D8_STAGES];                   // boxes of the stage whose page lies outside the pool, one bit each
+    int last;
+    alignas(16) float scale[D8_STAGES][2][D8_TILE / 16];    // scales of a stage's blocks, keys and values
+    uint64_t full[D8_STAGES], empty[D8_STAGES], q_full, q_empty;
+    uint32_t dead[D8_STAGES];                   // blocks of the stage whose page lies outside the pool, one bit each
 };
 
 struct D8Params {
@@ -89,16 +92,28 @@ struct D8Params {
     const float2* rope_table;
     float* part_ml;                             // [n_kv][parts + rows][G][2]: reference (log2 units), sum
     float* part_o;                              // [n_kv][parts + rows][G][DH]
+    unsigned* count;                            // [n_kv][parts], zero between calls
     int* status;
     int G, n_kv, T, interleaved, max_pos, box_rows;
+    unsigned page_magic;                        // see d8_page_of
     int rows;                                   // batch * T
+    int each;                                   // parts / rows, where a list has at most 128 rows
     int parts, least;                           // 0: a block per row and KV head; else parts of the list, of `least` steps at least
 };
 
+// Logical page of block b (of 16 tokens): b divided by the blocks of a page, with page_magic = 2^32 divided by them, rounded up.
+// b page_magic / 2^32 exceeds the quotient by less than b / 2^32 < 1.
+__device__ __forceinline__ int d8_page_of(const D8Params& p, int b) {
+    const int per = p.cv.page_size / LORC_BLOCK8;
+    if (per == 1) return b;
+    const int q = (int)__umulhi((unsigned)b, p.page_magic);
+    return q * per > b ? q - 1 : q;
+}
+
 // Row r = s T + t stands for query t of sequence s: the tokens up to that query's own (0: nothing to attend to).
 __device__ __forceinline__ int d8_len(const D8Params& p, int r, int* status) {
+    if (p.T == 1) return lorc_len8(p.cv, r, p.max_pos, status);
     const int s = r / p.T, len = lorc_len8(p.cv, s, p.max_pos, status);
-    if (p.T == 1) return len;
     if (len < p.T) {
         if (len > 0 && status) lorc_set_status(status, LORC_ERR_ARG);
         return 0;
@@ -108,63 +123,135 @@ __device__ __forceinline__ int d8_len(const D8Params& p, int r, int* status) {
 // Units of a row on the list; a row without tokens has one, in which its zeros are written.
 __device__ __forceinline__ int d8_weight(int len) { return len <= 0 ? 1 : (len - 1) / D8_UNIT + 1; }
 
-// Sum of the weights of rows [0, n); whole warps.
-__device__ __forceinline__ long long d8_total(const D8Params& p, int n, int lane) {
-    long long sum = 0;
-    for (int i = lane; i < n; i += 32) sum += d8_weight(d8_len(p, i, nullptr));
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    return sum;
-}
-__device__ __forceinline__ long long d8_per(const D8Params& p, long long total) {
-    const long long per = (total + p.parts - 1) / p.parts;
-    return per < p.least ? p.least : per;
-}
-
-// The row that holds step f of the list and the first step of that row; whole warps.
-__device__ __forceinline__ void d8_locate(const D8Params& p, long long f, int lane, int& row, long long& first) {
-    long long before = 0;
-    for (int i0 = 0; i0 < p.rows; i0 += 32) {
-        const int i = i0 + lane, w = i < p.rows ? d8_weight(d8_len(p, i, nullptr)) : 0;
-        long long end = w;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const long long x = __shfl_up_sync(0xffffffffu, end, o);
-            if (lane >= o) end += x;
-        }
-        const unsigned hit = __ballot_sync(0xffffffffu, f < before + end);
-        if (hit) {
-            const int l = __ffs(hit) - 1;
-            row = i0 + l;
-            first = before + __shfl_sync(0xffffffffu, end - w, l);
-            return;
-        }
-        before += __shfl_sync(0xffffffffu, end, 31);
-    }
-    row = p.rows;
-    first = before;
-}
-
-// What a block works on: steps [f, end) of the list, beginning in row `row`, whose first step is `first`.
+// What a block works on: units [f, end) of the list, beginning in row `row`, whose first unit is `first`; `per` units to a part.
+// Unit u of the list belongs to part base + u / per.  (The host sees to it that a list has fewer than 2^30 units.)
 struct D8Range {
-    long long f, end, first;
-    int row;
+    int f, end, first, row, per, base;
 };
+
+// Inclusive sums of w over the lanes.
+__device__ __forceinline__ int warp_sums(int w, int lane) {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, w, o);
+        if (lane >= o) w += x;
+    }
+    return w;
+}
+
+// By whole warps.  Up to 128 rows are loaded at once.
 __device__ __forceinline__ D8Range d8_range(const D8Params& p, int part, int lane) {
     D8Range r;
+    r.base = 0;
     if (p.parts == 0) {
         r.row = part;
         r.f = r.first = 0;
-        r.end = d8_weight(d8_len(p, part, nullptr));
+        r.end = r.per = d8_weight(d8_len(p, part, nullptr));
         return r;
     }
-    const long long total = d8_total(p, p.rows, lane), per = d8_per(p, total);
-    r.f = part * per;
-    r.end = r.f + per < total ? r.f + per : total;
+    int w[4], sum = 0;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) w[c] = c * 32 + lane < p.rows ? d8_weight(d8_len(p, c * 32 + lane, nullptr)) : 0;
+    for (int i = 128 + lane; i < p.rows; i += 32) sum += d8_weight(d8_len(p, i, nullptr));
+    const int total = __reduce_add_sync(0xffffffffu, sum + w[0] + w[1] + w[2] + w[3]);
+    r.per = max((int)((unsigned)(total + p.parts - 1) / (unsigned)p.parts), p.least);
+    if (p.each > 0) {
+        // as many parts for every row: each row is a list of its own
+        const int most = __reduce_max_sync(0xffffffffu, max(max(w[0], w[1]), max(w[2], w[3])));
+        const int longest = (int)((unsigned)(most + p.each - 1) / (unsigned)p.each);
+        if (longest <= r.per + max(r.per / 4, 2)) {
+            r.row = part / p.each;
+            r.base = r.row * p.each;
+            r.first = 0;
+            r.f = r.end = 0;
+            if (r.row < p.rows) {
+                const int mine = d8_weight(d8_len(p, r.row, nullptr));
+                r.per = max((int)((unsigned)(mine + p.each - 1) / (unsigned)p.each), p.least);
+                r.f = (part - r.base) * r.per;
+                r.end = min(r.f + r.per, mine);
+            }
+            return r;
+        }
+    }
+    r.f = part * r.per;
+    r.end = min(r.f + r.per, total);
     r.row = p.rows;
     r.first = 0;
-    if (r.f < r.end) d8_locate(p, r.f, lane, r.row, r.first);
+    if (r.f >= r.end) return r;
+    int before = 0;
+    bool found = false;
+    auto look = [&](int i0, int x) {             // rows i0 .. i0 + 31, lane's weight x
+        const int end = warp_sums(x, lane);
+        const unsigned hit = __ballot_sync(0xffffffffu, r.f < before + end);
+        if (hit) {
+            const int l = __ffs(hit) - 1;
+            r.row = i0 + l;
+            r.first = before + __shfl_sync(0xffffffffu, end - x, l);
+            found = true;
+        } else {
+            before += __shfl_sync(0xffffffffu, end, 31);
+        }
+    };
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+        if (!found && c * 32 < p.rows) look(c * 32, w[c]);
+    for (int i0 = 128; !found; i0 += 32) look(i0, i0 + lane < p.rows ? d8_weight(d8_len(p, i0 + lane, nullptr)) : 0);
     return r;
+}
+
+// Four numbers of the result: sums divided by the denominator.
+__device__ __forceinline__ void d8_store(const D8Params& p, long long at, const float4& acc, float L) {
+    const float inv = L != 0.f ? 1.f / L : 0.f;
+    const __nv_bfloat162 lo = __floats2bfloat162_rn(acc.x * inv, acc.y * inv), hi = __floats2bfloat162_rn(acc.z * inv, acc.w * inv);
+    *reinterpret_cast<uint2*>(p.out + at) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+    if (L == 0.f) lorc_set_status(p.status, LORC_ERR_EMPTY);
+}
+
+// Merge of a row that was cut into n pieces: the G heads of a KV head, by 128 threads, four dimensions each.  Pieces come four at a
+// time, and the sums so far are brought to a new reference with each four: one round trip to L2 per four pieces.
+template <int DH>
+__device__ __forceinline__ void d8_merge(const D8Params& p, long long unit0, int n, long long out0, int tid) {
+    for (int i = tid; i < p.G * (DH / 4); i += 128) {
+        const int h = i / (DH / 4), d = (i - h * (DH / 4)) * 4;
+        const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + unit0 + h;
+        const float* po = p.part_o + (unit0 + h) * DH + d;
+        float M = -INFINITY, L = 0.f;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int c0 = 0; c0 < n; c0 += 4) {
+            float2 x[4];
+            float4 y[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                x[c] = make_float2(0.f, 0.f);
+                y[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (c0 + c < n) {
+                    x[c] = __ldcg(ml + (long long)(c0 + c) * p.G);
+                    y[c] = __ldcg(reinterpret_cast<const float4*>(po + (long long)(c0 + c) * p.G * DH));
+                }
+            }
+            float now = M;
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                if (x[c].y != 0.f) now = fmaxf(now, x[c].x);
+            if (now > M) {
+                const float alpha = M == -INFINITY ? 0.f : exp2f(M - now);
+                L *= alpha;
+                acc.x *= alpha; acc.y *= alpha; acc.z *= alpha; acc.w *= alpha;
+                M = now;
+            }
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                if (x[c].y == 0.f) continue;
+                const float wgt = exp2f(x[c].x - M);
+                L += wgt * x[c].y;
+                acc.x += wgt * y[c].x;
+                acc.y += wgt * y[c].y;
+                acc.z += wgt * y[c].z;
+                acc.w += wgt * y[c].w;
+            }
+        }
+        d8_store(p, (out0 + h) * DH + d, acc, L);
+    }
 }
 
 template <int DH, bool E4M3>
@@ -180,9 +267,11 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
     const int G = p.G, H_q = G * p.n_kv;
     if (tid == 0) {
         for (int i = 0; i < D8_STAGES; ++i) {
-            mbar_init(&sm.full[i], 1);
+            mbar_init(&sm.full[i], 2);           // the copies, and the scales
             mbar_init(&sm.empty[i], 4);
         }
+        mbar_init(&sm.q_full, 1);
+        mbar_init(&sm.q_empty, 4);
         fence_barrier_init();
         prefetch_tensormap(&mapK);
         prefetch_tensormap(&mapV);
@@ -196,67 +285,162 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
     uint32_t par = 0;                            // and the parity of this round
 
     if (warp == 4) {
-        // ------------------------------------------------------------------ producer (one elected lane issues)
-        const int nbox = D8_TILE / p.box_rows;   // boxes per tile: 2, or up to 8 on small pages
-        int fetched = 0;                         // stages that may have copies under way
-        long long f = range.f, first = range.first;
-        for (int row = range.row; f < range.end && ok; ++row) {
-            const int s = row / p.T, len = d8_len(p, row, nullptr), w = d8_weight(len);
-            const long long stop = first + w < range.end ? first + w : range.end;
-            if (len <= 0) {
-                f = first += w;
-                continue;
+        // ------------------------------------------------------------------ producer (one elected lane issues the copies)
+        // Tiles of 128 tokens, row after row.  Lane b + 8 i looks up the page of block b and loads its scale (i = 0: keys, 1:
+        // values; other lanes idle): the page two tiles ahead, the scale while the tile's copies are under way.  A box in a page
+        // outside the pool (reported), or behind the end of the sequence, is fetched from behind the pool, where it reads as zero.
+        struct Tile {
+            int s, t0, t_end, page, y;           // page of this lane's block and the block's first row in it
+        };
+        const int nbox = D8_TILE / p.box_rows, blk = lane & 7;
+        const long long per_page = (cv.page_table ? cv.page_size : cv.seq_stride) / LORC_BLOCK8;
+        int f = range.f, first = range.first, row = range.row, len = 0;
+        Tile next = {0, 0, 0, 0, 0};
+        bool more = true;
+        // moves `next` to the tile behind it (before the first call: to the first one); more: there is one
+        auto advance = [&]() {
+            next.t0 += D8_TILE;
+            while (next.t0 >= next.t_end) {
+                if (len > 0) {                   // this row is done
+                    const int w = d8_weight(len);
+                    f = min(first + w, range.end);
+                    first += w;
+                    ++row;
+                }
+                for (; f < range.end; ++row) {
+                    len = d8_len(p, row, nullptr);
+                    if (len > 0) break;
+                    f = ++first;
+                }
+                if (f >= range.end) {
+                    more = false;
+                    return;
+                }
+                next.s = p.T == 1 ? row : row / p.T;
+                next.t0 = (f - first) * D8_UNIT;
+                next.t_end = min(len, (min(first + d8_weight(len), range.end) - first) * D8_UNIT);
             }
-            // lane i < nbox: the page of the tile's i-th box, -1 for a table entry outside the pool (reported).  Such a box,
-            // and one past the end of the sequence, is fetched from behind the pool, where it reads as zero.
-            auto lookup = [&](int t0) {
-                int page = cv.page_table ? cv.n_pages : 0;
-                if (cv.page_table != nullptr && lane < nbox && t0 + lane * p.box_rows < len) {
-                    page = cv.page_table[(long long)s * cv.max_pages_per_seq + (t0 + lane * p.box_rows) / cv.page_size];
-                    if (page < 0 || page >= cv.n_pages) {
-                        lorc_set_status(p.status, LORC_ERR_CAPACITY);
-                        page = -1;
-                    }
-                }
-                return page;
-            };
-            int t0 = (int)(f - first) * D8_UNIT;
-            const int t_end = min(len, (int)(stop - first) * D8_UNIT);
-            int mine = lookup(t0);
-            for (; t0 < t_end; t0 += D8_TILE) {
-                int pages[8];
-                const uint32_t dead = __ballot_sync(0xffffffffu, mine < 0);
-                if (mine < 0) mine = cv.n_pages;
+            // (looked at only when the tile's turn comes: the table access is under way until then)
+            const int pos = next.t0 + blk * LORC_BLOCK8;
+            next.page = next.s;
+            next.y = pos;
+            if (cv.page_table != nullptr) {
+                const int lp = d8_page_of(p, pos / LORC_BLOCK8);
+                next.page = cv.n_pages;
+                next.y = pos - lp * cv.page_size;
+                if (lane < 16 && pos < next.t_end) next.page = cv.page_table[(long long)next.s * cv.max_pages_per_seq + lp];
+            }
+        };
+        Tile now;
+        float scale = 0.f, before = 0.f;         // this lane's scale of the tile, and of the one before
+        int fetched = 0, prev = -1;              // stages that may have copies under way; the stage that `before` belongs to
+        advance();
+        bool live = more;
+        now = next;
+        if (live) advance();
+        while (live) {
+            // All that a tile needs is known before its stage is free: the time from there to the copies counts.  (With the
+            // divisions of the page arithmetic behind the wait, 64 x 8448 tokens in 64-token pages took 219 us, now 174.)
+            const bool bad = cv.page_table != nullptr && lane < 16 && now.t0 + blk * LORC_BLOCK8 < now.t_end &&
+                             (now.page < 0 || now.page >= cv.n_pages);
+            if (bad) lorc_set_status(p.status, LORC_ERR_CAPACITY);
+            const uint32_t dead = __ballot_sync(0xffffffffu, bad) & 0xff;
+            const int boxes = min(nbox, (now.t_end - now.t0 + p.box_rows - 1) / p.box_rows);      // (the others are not fetched)
+            int z[8], y[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) pages[j] = __shfl_sync(0xffffffffu, mine, j);
-                if (t0 + D8_TILE < t_end) mine = lookup(t0 + D8_TILE);
-                ok = __all_sync(0xffffffffu, mbar_wait(&sm.empty[st], par ^ 1));
-                if (!ok) break;
-                if (elect_one()) {
-                    // boxes wholly behind the part's end are not fetched
-                    const int live = min(nbox, (t_end - t0 + p.box_rows - 1) / p.box_rows);
-                    sm.dead[st] = dead;
-                    mbar_arrive_expect_tx(&sm.full[st], 2 * DH * p.box_rows * live);
+            for (int j = 0; j < 8; ++j) {
+                z[j] = __shfl_sync(0xffffffffu, bad ? cv.n_pages : now.page, j * p.box_rows / LORC_BLOCK8 & 7);
+                y[j] = __shfl_sync(0xffffffffu, now.y, j * p.box_rows / LORC_BLOCK8 & 7);
+            }
+            scale = 0.f;
+            if (lane < 16 && now.t0 + blk * LORC_BLOCK8 < now.t_end && !bad) {
+                const long long at = (long long)now.page * per_page + now.y / LORC_BLOCK8;
+                scale = (lane < 8 ? cv.k_scale : cv.v_scale)[at * p.n_kv + kvh];
+            }
+            ok = __all_sync(0xffffffffu, mbar_wait(&sm.empty[st], par ^ 1));
+            if (!ok) break;
+            if (elect_one()) {
+                sm.dead[st] = dead;
+                mbar_arrive_expect_tx(&sm.full[st], 2 * DH * p.box_rows * boxes);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        if (j >= live) break;
-                        const int tok = t0 + j * p.box_rows;
-                        const int y = cv.page_table ? tok % cv.page_size : tok, z = cv.page_table ? pages[j] : s;
-                        tma_load_3d(sm.kv[st][0] + j * p.box_rows * DH, &mapK, &sm.full[st], kvh * DH, y, z);
-                        tma_load_3d(sm.kv[st][1] + j * p.box_rows * DH, &mapV, &sm.full[st], kvh * DH, y, z);
-                    }
+                for (int j = 0; j < 8; ++j) {
+                    if (j >= boxes) break;
+                    tma_load_3d(sm.kv[st][0] + j * p.box_rows * DH, &mapK, &sm.full[st], kvh * DH, y[j], z[j]);
+                    tma_load_3d(sm.kv[st][1] + j * p.box_rows * DH, &mapV, &sm.full[st], kvh * DH, y[j], z[j]);
                 }
+            }
+            __syncwarp();
+            if (prev >= 0) {                     // the scales of the tile before have come
+                if (lane < 16) sm.scale[prev][lane >> 3][blk] = before;
                 __syncwarp();
-                if (++st == D8_STAGES) { st = 0; par ^= 1; }
-                if (fetched < D8_STAGES) ++fetched;
+                if (lane == 0) mbar_arrive(&sm.full[prev]);
             }
-            f = stop;
-            first += w;
+            before = scale;
+            prev = st;
+            live = more;
+            now = next;
+            if (more) advance();
+            if (++st == D8_STAGES) { st = 0; par ^= 1; }
+            if (fetched < D8_STAGES) ++fetched;
+        }
+        if (prev >= 0) {
+            if (lane < 16) sm.scale[prev][lane >> 3][blk] = before;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sm.full[prev]);
         }
         // The block stays until the copies into its shared memory have landed, also when a wait has run out.
         for (; fetched > 0; --fetched) {
             if (--st < 0) { st = D8_STAGES - 1; par ^= 1; }
             if (!mbar_wait(&sm.full[st], par)) ok = false;
+        }
+        if (!ok && lane == 0) lorc_set_status(p.status, LORC_ERR_TIMEOUT);
+        return;
+    }
+    if (warp == 5) {
+        // ------------------------------------------------------------------ queries: RoPE(q, position) of the G heads, one row ahead
+        constexpr int E = DH / 64;               // rotary pairs per lane
+        int f = range.f, first = range.first;
+        for (int row = range.row; f < range.end && ok; ++row) {
+            const int len = d8_len(p, row, nullptr), w = d8_weight(len);
+            if (len > 0) {
+                const bf16* q = p.q + ((long long)row * H_q + kvh * G) * DH;
+                const float2* cs = p.rope_table + (long long)(len - 1) * (DH / 2) + lane * E;
+                int ia[E], ib[E];
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    ia[e] = p.interleaved ? 2 * (lane * E + e) : lane * E + e;
+                    ib[e] = p.interleaved ? ia[e] + 1 : ia[e] + DH / 2;
+                }
+                bf16 a[8][E], b[8][E];
+                float2 c[E];
+#pragma unroll
+                for (int h = 0; h < 8; ++h)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        a[h][e] = b[h][e] = __float2bfloat16_rn(0.f);
+                        if (h < G) {
+                            a[h][e] = q[h * DH + ia[e]];
+                            b[h][e] = q[h * DH + ib[e]];
+                        }
+                    }
+#pragma unroll
+                for (int e = 0; e < E; ++e) c[e] = cs[e];
+                ok = __all_sync(0xffffffffu, mbar_wait(&sm.q_empty, par ^ 1));
+                if (!ok) break;
+#pragma unroll
+                for (int h = 0; h < 8; ++h)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        const float x = __bfloat162float(a[h][e]), y = __bfloat162float(b[h][e]);
+                        sm.qs[h][ia[e]] = x * c[e].x - y * c[e].y;
+                        sm.qs[h][ib[e]] = x * c[e].y + y * c[e].x;
+                    }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sm.q_full);
+                par ^= 1;
+            }
+            first += w;
+            f = min(first, range.end);
         }
         if (!ok && lane == 0) lorc_set_status(p.status, LORC_ERR_TIMEOUT);
         return;
@@ -268,45 +452,18 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
     const int mi = lane >> 3, lr = lane & 7;
     const uint32_t my_row = (uint32_t)(warp * 32 + (mi & 1) * 8 + lr);
     const uint32_t row_off = my_row * DH, sw = DH == 128 ? my_row & 7 : (my_row >> 1) & 3;
-    const int box0 = warp * 32 / p.box_rows, box1 = (warp * 32 + 16) / p.box_rows;      // the boxes of this warp's tokens
-    long long f = range.f, first = range.first;
+    uint32_t q_par = 0;
+    int f = range.f, first = range.first;
     for (int row = range.row; f < range.end; ++row) {
-        const int s = row / p.T, len = d8_len(p, row, tid == 0 ? p.status : nullptr), w = d8_weight(len);
-        const long long stop = first + w < range.end ? first + w : range.end;
+        const int len = d8_len(p, row, tid == 0 ? p.status : nullptr), w = d8_weight(len);
+        const int stop = min(first + w, range.end);
         const bool whole = f == first && stop == first + w;
-        const int t_begin = (int)(f - first) * D8_UNIT, t_end = min(len, (int)(stop - first) * D8_UNIT);
+        const int t_begin = (f - first) * D8_UNIT, t_end = min(len, (stop - first) * D8_UNIT);
 
-        // the scales of this warp's blocks, two a step, 16 steps at a time: lane 2 j + u holds block u of step j
-        auto scales = [&](int t0, float& ks, float& vs) {
-            const int pos = t0 + (lane >> 1) * D8_TILE + warp * 32 + (lane & 1) * 16;
-            ks = vs = 0.f;
-            if (pos < t_end) {
-                const long long at = lorc_block8(cv, s, pos / LORC_BLOCK8);
-                if (at >= 0) {
-                    ks = cv.k_scale[at * p.n_kv + kvh];
-                    vs = cv.v_scale[at * p.n_kv + kvh];
-                }
-            }
-        };
-        float ks_now, vs_now, ks_next = 0.f, vs_next = 0.f;
-        scales(t_begin, ks_now, vs_now);
-
-        // RoPE(q, position) for the G heads of this KV head
-        for (int i = tid; i < 8 * (DH / 2); i += 128) {
-            const int h = i / (DH / 2), jj = i - h * (DH / 2);
-            const int ia = p.interleaved ? 2 * jj : jj, ib = p.interleaved ? 2 * jj + 1 : jj + DH / 2;
-            float ra = 0.f, rb = 0.f;
-            if (h < G && len > 0) {
-                const bf16* qp = p.q + ((long long)row * H_q + kvh * G + h) * DH;
-                const float a = __bfloat162float(qp[ia]), b = __bfloat162float(qp[ib]);
-                const float2 cs = p.rope_table[(long long)(len - 1) * (DH / 2) + jj];
-                ra = a * cs.x - b * cs.y;
-                rb = a * cs.y + b * cs.x;
-            }
-            sm.qs[h][ia] = ra;
-            sm.qs[h][ib] = rb;
+        if (len > 0) {
+            if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&sm.q_full, q_par));
+            q_par ^= 1;
         }
-        asm volatile("bar.sync 1, 128;" ::: "memory");
         // Query fragments of head g: piece ks, dimensions 4 t .. 4 t + 3 of its 16.
         uint32_t qhi[KS][2], qlo[KS][2];
         float factor[2];                         // heads 2 t, 2 t + 1: what brings a sum of code products to log2 units
@@ -332,6 +489,8 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
                 qlo[ks][0] = pack_half(v.x - a.x, v.y - a.y);
                 qlo[ks][1] = pack_half(v.z - b.x, v.w - b.y);
             }
+            __syncwarp();
+            if (len > 0 && lane == 0) mbar_arrive(&sm.q_empty);
             const float base = rsqrtf((float)DH) * LOG2E;
             factor[0] = __shfl_sync(0xffffffffu, up, 8 * t) * base;
             factor[1] = __shfl_sync(0xffffffffu, up, 8 * t + 4) * base;
@@ -342,21 +501,14 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
         float m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};   // heads 2 t, 2 t + 1 (l: this lane's tokens)
         float v_ref = 0.f, v_inv = 0.f;          // largest scale of values so far: o is in units of it
 
-        int turn = 0;
-        for (int t0 = t_begin; t0 < t_end && ok; t0 += D8_TILE, turn = (turn + 2) & 31) {
+        for (int t0 = t_begin; t0 < t_end && ok; t0 += D8_TILE) {
             const int tw = t0 + warp * 32;       // first token of this warp
-            if (turn == 0) {
-                if (t0 > t_begin) { ks_now = ks_next; vs_now = vs_next; }
-                if (t0 + 16 * D8_TILE < t_end) scales(t0 + 16 * D8_TILE, ks_next, vs_next);
-            }
-            float k_scale[2], v_scale[2];
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                k_scale[u] = __shfl_sync(0xffffffffu, ks_now, turn + u);
-                v_scale[u] = __shfl_sync(0xffffffffu, vs_now, turn + u);
-            }
             ok = __all_sync(0xffffffffu, mbar_wait(&sm.full[st], par));
             if (!ok) break;
+            const float2 k_scale2 = *reinterpret_cast<const float2*>(&sm.scale[st][0][2 * warp]);
+            const float2 v_scale2 = *reinterpret_cast<const float2*>(&sm.scale[st][1][2 * warp]);
+            const float k_scale[2] = {k_scale2.x, k_scale2.y};
+            float v_scale[2] = {v_scale2.x, v_scale2.y};
             const uint32_t k0 = smem_u32(sm.kv[st][0]) + row_off, v0 = smem_u32(sm.kv[st][1]) + row_off;
             // scores of tokens g, g + 8 of both blocks against heads 2 t, 2 t + 1
             float x[2][4];
@@ -386,7 +538,7 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
             if (tw + 32 > t_end || dead) {       // tokens past the end, or in pages that do not exist
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    const int live = (dead >> (u ? box1 : box0)) & 1 ? 0 : t_end - tw - 16 * u;
+                    const int live = (dead >> (2 * warp + u)) & 1 ? 0 : t_end - tw - 16 * u;
                     if (live <= 0) v_scale[u] = 0.f;
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
@@ -484,70 +636,51 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
                         *reinterpret_cast<float2*>(&sm.o[warp][2 * t + e - h0][16 * ks + 2 * g]) = make_float2(o[ks][e], o[ks][2 + e]);
             __syncwarp();
             asm volatile("bar.sync 1, 128;" ::: "memory");
-            const int heads = min(G - h0, 4);
-            for (int i = tid; i < heads * DH; i += 128) {
-                const int h = h0 + i / DH, d = i % DH;
+            const int h = h0 + tid / (DH / 4), d = tid % (DH / 4) * 4;          // a thread takes four dimensions of a head
+            if (h < min(G, h0 + 4)) {
                 float M = -INFINITY;
 #pragma unroll
                 for (int x = 0; x < 4; ++x)
                     if (sm.l[x][h] != 0.f) M = fmaxf(M, sm.m[x][h]);
-                float L = 0.f, acc = 0.f;
+                float L = 0.f;
+                float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
-                    const float wgt = sm.l[x][h] != 0.f ? exp2f(sm.m[x][h] - M) : 0.f;
+                    const float wgt = sm.l[x][h] != 0.f ? exp2f(sm.m[x][h] - M) : 0.f, c = wgt * sm.vs[x];
+                    const float4 y = *reinterpret_cast<const float4*>(&sm.o[x][h - h0][d]);
                     L += wgt * sm.l[x][h];
-                    acc += wgt * sm.vs[x] * sm.o[x][h - h0][d];
+                    acc.x += c * y.x;
+                    acc.y += c * y.y;
+                    acc.z += c * y.z;
+                    acc.w += c * y.w;
                 }
                 if (whole) {
-                    p.out[((long long)row * H_q + kvh * G + h) * DH + d] = __float2bfloat16_rn(L != 0.f ? acc / L : 0.f);
-                    if (L == 0.f && d == 0) lorc_set_status(p.status, LORC_ERR_EMPTY);
+                    d8_store(p, ((long long)row * H_q + kvh * G + h) * DH + d, acc, L);
                 } else {
                     const long long unit = ((long long)kvh * (p.parts + p.rows) + part + row) * G + h;
                     if (d == 0) *reinterpret_cast<float2*>(p.part_ml + unit * 2) = make_float2(M, L);
-                    p.part_o[unit * DH + d] = acc;
+                    *reinterpret_cast<float4*>(p.part_o + unit * DH + d) = acc;
                 }
             }
             if (h0 + 4 < G) asm volatile("bar.sync 1, 128;" ::: "memory");
+        }
+        if (!whole) {
+            // The row's parts c0 .. c1 count themselves in (the counter of c0, since a part begins at most one row that it does not
+            // end); the last one adds up all pieces, in their order, and leaves the counter at zero.
+            const int c0 = range.base + first / range.per, c1 = range.base + (first + w - 1) / range.per, n = c1 - c0 + 1;
+            __threadfence();
+            asm volatile("bar.sync 1, 128;" ::: "memory");
+            if (tid == 0) sm.last = atomicInc(p.count + kvh * p.parts + c0, n - 1) == (unsigned)(n - 1);
+            asm volatile("bar.sync 1, 128;" ::: "memory");
+            if (sm.last) {
+                __threadfence();
+                d8_merge<DH>(p, ((long long)kvh * (p.parts + p.rows) + c0 + row) * G, n, (long long)row * H_q + kvh * G, tid);
+            }
         }
         first += w;
         f = stop;
     }
     if (!ok && lane == 0) lorc_set_status(p.status, LORC_ERR_TIMEOUT);
-}
-
-// Sequences that were cut: piece i of row r came from part c0 + i and lies in slot c0 + i + r.  One block per (head, row).
-template <int DH>
-__global__ void __launch_bounds__(DH)
-decode8_merge_kernel(const D8Params p) {
-    const int tid = threadIdx.x, lane = tid & 31;
-    const int H_q = p.G * p.n_kv, hq = (int)blockIdx.x % H_q, row = (int)blockIdx.x / H_q, kvh = hq / p.G, h = hq - kvh * p.G;
-    grid_dep_wait();
-    grid_dep_launch();
-    const long long per = d8_per(p, d8_total(p, p.rows, lane)), first = d8_total(p, row, lane);
-    const int w = d8_weight(d8_len(p, row, nullptr));
-    const int c0 = (int)(first / per), c1 = (int)((first + w - 1) / per);
-    if (c0 == c1) return;                        // one block had it all and has written the result
-    const long long unit0 = ((long long)kvh * (p.parts + p.rows) + c0 + row) * p.G + h;
-    const int n = c1 - c0 + 1;
-    float M = -INFINITY;
-    for (int c = lane; c < n; c += 32) {
-        const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + (unit0 + (long long)c * p.G) * 2);
-        if (ml.y != 0.f) M = fmaxf(M, ml.x);
-    }
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-    float L = 0.f, acc = 0.f;
-#pragma unroll 4
-    for (int c = 0; c < n; ++c) {
-        const long long unit = unit0 + (long long)c * p.G;
-        const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + unit * 2);
-        const float x = p.part_o[unit * DH + tid];
-        const float wgt = ml.y != 0.f ? exp2f(ml.x - M) : 0.f;
-        L += wgt * ml.y;
-        acc += wgt != 0.f ? wgt * x : 0.f;
-    }
-    p.out[((long long)row * H_q + hq) * DH + tid] = __float2bfloat16_rn(L != 0.f ? acc / L : 0.f);
-    if (L == 0.f && tid == 0) lorc_set_status(p.status, LORC_ERR_EMPTY);
 }
 
 // 8-bit rows in boxes of d_head bytes x box_rows tokens.
@@ -567,7 +700,7 @@ bool make_map8(CUtensorMap* map, const void* base, const Cache8View& cv, int dh,
 // at most four steps long, or, with several queries per sequence, where there are more rows than parts (they are about equally
 // long then, and the list would be long to search).
 void d8_plan(const lorc_ctx* ctx, int rows, int max_seq_len, int T, int* parts, int* least) {
-    const int slots = D8_BLOCKS_PER_SM * ctx->sm_count / ctx->desc.n_kv_heads;
+    const int slots = D8_BLOCKS_PER_SM * ctx->sm_count / ctx->desc.n_kv_heads;      // (lorc_part_counters goes by this)
     *parts = slots > 1 ? slots : 1;
     *least = 2;
     if (max_seq_len <= 4 * D8_UNIT || (T > 1 && rows >= *parts)) *parts = 0;
@@ -613,24 +746,18 @@ cudaError_t lorc_decode8_launch(lorc_ctx* ctx, const Cache8View& cv, const bf16*
     if (!make_map8(&mapK, cv.k, cv, d.d_head, box_rows) || !make_map8(&mapV, cv.v, cv, d.d_head, box_rows)) return cudaErrorInvalidValue;
     D8Params p;
     p.q = q; p.out = out; p.cv = cv; p.rope_table = ctx->rope_table; p.status = ctx->status_dev;
+    p.count = ctx->part_count;
     p.G = ctx->group; p.n_kv = d.n_kv_heads; p.T = T; p.interleaved = ctx->pair_style == LORC_ROPE_INTERLEAVED;
     p.max_pos = d.max_pos; p.box_rows = box_rows; p.rows = cv.batch * T;
+    const unsigned per = cv.page_table ? cv.page_size / LORC_BLOCK8 : 1;
+    p.page_magic = per > 1 ? (unsigned)(((1ull << 32) + per - 1) / per) : 0;
     d8_plan(ctx, p.rows, cv.max_seq_len, T, &p.parts, &p.least);
+    p.each = p.rows <= 128 ? p.parts / p.rows : 0;
     p.part_ml = (float*)scratch;
     p.part_o = (float*)((char*)scratch + d8_ml_bytes(ctx, p.parts + p.rows));
     const bool e4m3 = cv.type == LORC_CACHE8_E4M3;
-    cudaError_t e;
-    {
-        LorcStageTimer timer(ctx, LORC_STAGE_SCORE, st);
-        e = d.d_head == 128 ? (e4m3 ? d8_launch<128, true>(ctx, mapK, mapV, p, st) : d8_launch<128, false>(ctx, mapK, mapV, p, st))
-                            : (e4m3 ? d8_launch<64, true>(ctx, mapK, mapV, p, st) : d8_launch<64, false>(ctx, mapK, mapV, p, st));
-        *launches += 1;
-    }
-    if (e != cudaSuccess || p.parts == 0) return e;
-    LorcStageTimer timer(ctx, LORC_STAGE_COMBINE, st);
-    const long long blocks = (long long)p.rows * d.n_q_heads;
-    if (blocks > 0x7fffffffll) return cudaErrorInvalidValue;
+    LorcStageTimer timer(ctx, LORC_STAGE_SCORE, st);
     *launches += 1;
-    return d.d_head == 128 ? lorc_launch_dependent(decode8_merge_kernel<128>, dim3((unsigned)blocks), dim3(128), 0, st, p)
-                           : lorc_launch_dependent(decode8_merge_kernel<64>, dim3((unsigned)blocks), dim3(64), 0, st, p);
+    return d.d_head == 128 ? (e4m3 ? d8_launch<128, true>(ctx, mapK, mapV, p, st) : d8_launch<128, false>(ctx, mapK, mapV, p, st))
+                           : (e4m3 ? d8_launch<64, true>(ctx, mapK, mapV, p, st) : d8_launch<64, false>(ctx, mapK, mapV, p, st));
 }

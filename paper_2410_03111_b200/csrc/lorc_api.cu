@@ -154,6 +154,9 @@ int lorc_create(const lorc_model_desc* desc, lorc_ctx** out) {
         e = cudaDeviceGetAttribute(&ctx->sm_count, cudaDevAttrMultiProcessorCount, ctx->device);
     if (e == cudaSuccess) e = cudaMalloc(&ctx->status_dev, sizeof(int));
     if (e == cudaSuccess) e = cudaMemset(ctx->status_dev, 0, sizeof(int));
+    const size_t counters = lorc_part_counters(ctx->sm_count, desc->n_kv_heads) * sizeof(unsigned);
+    if (e == cudaSuccess) e = cudaMalloc(&ctx->part_count, counters);
+    if (e == cudaSuccess) e = cudaMemset(ctx->part_count, 0, counters);
     size_t tbytes = (size_t)desc->max_pos * (desc->d_head / 2) * sizeof(float2);
     if (e == cudaSuccess) e = cudaMalloc(&ctx->rope_table, tbytes);
     if (e == cudaSuccess)
@@ -162,6 +165,7 @@ int lorc_create(const lorc_model_desc* desc, lorc_ctx** out) {
     if (e == cudaSuccess) e = cudaDeviceSynchronize();
     if (e != cudaSuccess) {
         cudaFree(ctx->status_dev);
+        cudaFree(ctx->part_count);
         cudaFree(ctx->rope_table);
         delete ctx->prof;
         delete ctx;
@@ -184,6 +188,7 @@ int lorc_destroy(lorc_ctx* ctx) {
         delete ctx->prof;
     }
     cudaFree(ctx->status_dev);
+    cudaFree(ctx->part_count);
     cudaFree(ctx->rope_table);
     delete ctx;
     return LORC_OK;
