@@ -1,11 +1,11 @@
 // Cache write of uncompressed layers in 8 bits: [K | V] = x [W_k | W_v], keys rotated, both rounded to codes with one scale per
-// block of 16 tokens and KV head.
+// block of 16 tokens and KV head.  Prompt-sized launches run in append8_tc.cu; here are the others.
 //
 // Two kernels.  The projection leaves fp32 numbers [tokens][2 n] in the workspace; the second kernel has a block of threads for each
 // (block of tokens, KV head, keys or values), which sees all numbers that share a scale.
 #include <math.h>
 
-#include "cache8.cuh"
+#include "append8.cuh"
 #include "sm100_ptx.cuh"
 #include "tc_kernels.cuh"
 
@@ -120,52 +120,31 @@ project8_plain_kernel(const bf16* __restrict__ x, const bf16* __restrict__ A_cat
 // rotation and quantisation: grid (batch * blocks a chunk can reach, KV heads, keys / values); 16 threads of 16 bytes per row of 128
 // dimensions are eight, so 128 (64) threads are the 16 rows.  A thread owns 16 dimensions of a row: one 16-byte store.
 // ---------------------------------------------------------------------------------------------
-struct Quant8Params {
-    const float* proj;
-    Cache8View cv;
-    const float2* rope_table;
-    int* status;
-    int T, n_blocks, max_pos, interleaved, pairs_adjacent;     // pairs_adjacent: see the key columns of retile_factor_kernel
-};
-
 template <int DH, bool E4M3>
 __global__ void __launch_bounds__(DH)
-quantize8_kernel(const Quant8Params p) {
+quantize8_kernel(const Append8Params p, const float* __restrict__ proj, int pairs_adjacent) {
     constexpr int TPR = DH / 16, WARPS = DH / 32;
     __shared__ float most_s[WARPS];
-    __shared__ int flags_s[WARPS];
+    __shared__ int odd_s[WARPS];
     const Cache8View& cv = p.cv;
     const int tid = threadIdx.x, r = tid / TPR, d0 = (tid % TPR) * 16;
     const int s = (int)blockIdx.x / p.n_blocks, head = blockIdx.y;
     const bool val = blockIdx.z != 0;
     grid_dep_wait();
     grid_dep_launch();
-    const int len = cv.seq_lens[s], first = len - p.T;
-    // a sequence that is too long, or shorter than what is written to it, is reported; of the latter the tokens that have a place
-    // are written
-    const bool fits = len <= cv.max_seq_len && len <= p.max_pos && len <= cv.capacity;
-    if ((!fits || first < 0) && tid == 0) lorc_set_status(p.status, LORC_ERR_CAPACITY);
-    if (!fits) return;
-    const int begin = max(first, 0);
-    const int blk = begin / LORC_BLOCK8 + (int)blockIdx.x % p.n_blocks;
-    if (blk * LORC_BLOCK8 >= len) return;
-    const long long at = lorc_block8(cv, s, blk);
-    if (at < 0) {
-        if (tid == 0) lorc_set_status(p.status, LORC_ERR_CAPACITY);
-        return;
-    }
-    const int pos = blk * LORC_BLOCK8 + r;
-    const bool fresh = pos >= begin && pos < len, old = pos < begin;
+    Append8Row row;
+    append8_row(p, s, (int)blockIdx.x % p.n_blocks, r, row);
+    if (row.at < 0) return;                      // (the whole block of threads)
     float x[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i] = 0.f;
-    if (fresh) {
-        const float* src = p.proj + ((long long)s * p.T + (pos - first)) * (2 * cv.n) + (val ? cv.n : 0) + head * DH;
+    if (row.fresh) {
+        const float* src = proj + ((long long)s * p.T + (row.pos - (cv.seq_lens[s] - p.T))) * (2 * cv.n) + (val ? cv.n : 0) + head * DH;
         if (val) {
 #pragma unroll
             for (int i = 0; i < 16; i += 4) *reinterpret_cast<float4*>(x + i) = *reinterpret_cast<const float4*>(src + d0 + i);
         } else {
-            const float2* cs = p.rope_table + (long long)pos * (DH / 2);
+            const float2* cs = p.rope_table + (long long)row.pos * (DH / 2);
             if (p.interleaved) {
 #pragma unroll
                 for (int i = 0; i < 16; i += 2) {
@@ -179,71 +158,56 @@ quantize8_kernel(const Quant8Params p) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const int j = j0 + i;
-                    const float a = src[p.pairs_adjacent ? 2 * j : j], b = src[p.pairs_adjacent ? 2 * j + 1 : j + DH / 2];
+                    const float a = src[pairs_adjacent ? 2 * j : j], b = src[pairs_adjacent ? 2 * j + 1 : j + DH / 2];
                     const float2 c = cs[j];
                     x[i] = second ? a * c.y + b * c.x : a * c.x - b * c.y;
                 }
             }
         }
     }
-    // largest magnitude of the new numbers; what is not finite does not count
-    float most = 0.f;
     bool odd = false;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const float m = fabsf(x[i]);
-        if (m <= 3.4028234663852886e38f) most = fmaxf(most, m);
-        else odd = true;
-    }
+    float most = append8_most(x, odd);
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
     const int any_odd = __any_sync(0xffffffffu, odd);
     if ((tid & 31) == 0) {
         most_s[tid >> 5] = most;
-        flags_s[tid >> 5] = any_odd;
+        odd_s[tid >> 5] = any_odd;
     }
-    // the scale so far, where earlier tokens stand under it.  (Read by all threads before the barrier, written by one behind it.)
-    float* scale_at = (val ? cv.v_scale : cv.k_scale) + at * cv.n_kv + head;
-    float before = begin > blk * LORC_BLOCK8 ? *scale_at : 0.f;
-    before = before > 0.f ? before : 0.f;
+    // (read by all threads before the barrier, written by one behind it)
+    float* scale_at = (val ? cv.v_scale : cv.k_scale) + row.at * cv.n_kv + head;
+    const float before = row.has_old ? *scale_at : 0.f;
     __syncthreads();
-#pragma unroll
-    for (int w = 0; w < WARPS; ++w) most = fmaxf(most, most_s[w]);
     int bad = 0;
 #pragma unroll
-    for (int w = 0; w < WARPS; ++w) bad |= flags_s[w];
-    const float scale = fmaxf(lorc_scale8<E4M3>(most), before);
+    for (int w = 0; w < WARPS; ++w) {
+        most = fmaxf(most, most_s[w]);
+        bad |= odd_s[w];
+    }
+    const float scale = append8_scale<E4M3>(most, before);
     if (tid == 0) {
         *scale_at = scale;
         if (bad) lorc_set_status(p.status, LORC_ERR_ARG);
     }
-    uint4* dst = reinterpret_cast<uint4*>((val ? cv.v : cv.k) + (at * LORC_BLOCK8 + r) * cv.n + head * DH + d0);
-    uint32_t w[4];
-    if (fresh) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            w[i] = lorc_to_codes2<E4M3>(x[4 * i] / scale, x[4 * i + 1] / scale) |
-                   lorc_to_codes2<E4M3>(x[4 * i + 2] / scale, x[4 * i + 3] / scale) << 16;
-        *dst = make_uint4(w[0], w[1], w[2], w[3]);
-    } else if (old && scale != before) {
-        const float keep = before / scale;
-        const uint4 c = *dst;
-        const uint32_t in[4] = {c.x, c.y, c.z, c.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint32_t a, b;
-            lorc_codes_half<E4M3, 0, 1, 2, 3>(in[i], a, b);
-            const float2 u = __half22float2(*reinterpret_cast<__half2*>(&a)), v = __half22float2(*reinterpret_cast<__half2*>(&b));
-            w[i] = lorc_to_codes2<E4M3>(u.x * keep, u.y * keep) | lorc_to_codes2<E4M3>(v.x * keep, v.y * keep) << 16;
-        }
-        *dst = make_uint4(w[0], w[1], w[2], w[3]);
-    }
+    uint4* dst = reinterpret_cast<uint4*>((val ? cv.v : cv.k) + (row.at * LORC_BLOCK8 + r) * cv.n + head * DH + d0);
+    if (row.fresh) *dst = append8_codes<E4M3>(x, 1.f / scale, false);
+    else if (row.old && scale != before) *dst = append8_recode<E4M3>(*dst, (before > 0.f ? before : 0.f) / scale);
 }
 
 }  // namespace
 
 size_t lorc_append8_scratch_bytes(const lorc_ctx* ctx, int batch, int T) {
+    if (lorc_append8_tc_supported(ctx, batch, T)) return 0;
     return lorc_align_up((size_t)batch * T * 2 * ctx->n * sizeof(float), 256);
+}
+
+size_t lorc_append8_scratch_most(const lorc_ctx* ctx, int batch, int T) {
+    // a call with fewer tokens may run on the other kernels
+    const long long all = (long long)batch * T;
+    long long n = all;
+    if (lorc_append8_tc_supported(ctx, batch, T))
+        for (n = 0; n + 16 <= all && !lorc_append8_tc_supported(ctx, 1, (int)n + 16);) n += 16;
+    return lorc_align_up((size_t)n * 2 * ctx->n * sizeof(float), 256);
 }
 
 cudaError_t lorc_append8_launch(lorc_ctx* ctx, const LorcLayer& L, const Cache8View& cv, const bf16* x, int T, void* scratch,
@@ -251,6 +215,11 @@ cudaError_t lorc_append8_launch(lorc_ctx* ctx, const LorcLayer& L, const Cache8V
     const int D = ctx->desc.d_model, R = 2 * ctx->n;
     const long long n_tok = (long long)cv.batch * T;
     float* proj = (float*)scratch;
+    Append8Params p;
+    p.cv = cv; p.rope_table = ctx->rope_table; p.status = ctx->status_dev; p.T = T; p.max_pos = ctx->desc.max_pos;
+    p.n_blocks = (T + LORC_BLOCK8 - 2) / LORC_BLOCK8 + 1;
+    p.interleaved = ctx->pair_style == LORC_ROPE_INTERLEAVED;
+    if (lorc_append8_tc_supported(ctx, cv.batch, T)) return lorc_append8_tc_launch(ctx, L, p, x, st, launches);
     const bool mma = D % 256 == 0 && L.A_tiled != nullptr;
     // grid rows are limited to 65535: chunks of as many tokens
     const int tile = mma ? 16 : 8;
@@ -266,16 +235,12 @@ cudaError_t lorc_append8_launch(lorc_ctx* ctx, const LorcLayer& L, const Cache8V
         *launches += 1;
         if (e != cudaSuccess) return e;
     }
-    Quant8Params p;
-    p.proj = proj; p.cv = cv; p.rope_table = ctx->rope_table; p.status = ctx->status_dev; p.T = T; p.max_pos = ctx->desc.max_pos;
-    p.n_blocks = (T + LORC_BLOCK8 - 2) / LORC_BLOCK8 + 1;
-    p.interleaved = ctx->pair_style == LORC_ROPE_INTERLEAVED;
-    p.pairs_adjacent = mma && ctx->pair_style == LORC_ROPE_HALF_SPLIT;
+    const int adjacent = mma && ctx->pair_style == LORC_ROPE_HALF_SPLIT;
     const dim3 grid((unsigned)((long long)cv.batch * p.n_blocks), (unsigned)cv.n_kv, 2);
     const int DH = ctx->desc.d_head;
     const bool e4m3 = cv.type == LORC_CACHE8_E4M3;
     auto kernel = DH == 128 ? (e4m3 ? quantize8_kernel<128, true> : quantize8_kernel<128, false>)
                             : (e4m3 ? quantize8_kernel<64, true> : quantize8_kernel<64, false>);
     *launches += 1;
-    return lorc_launch_dependent(kernel, grid, dim3(DH), 0, st, p);
+    return lorc_launch_dependent(kernel, grid, dim3(DH), 0, st, p, (const float*)proj, adjacent);
 }

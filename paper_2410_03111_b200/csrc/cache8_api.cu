@@ -97,7 +97,7 @@ extern "C" {
 
 size_t lorc_cache8_workspace_bytes(const lorc_ctx* ctx, int batch, int max_seq_len, int T) {
     if (!ctx || batch <= 0 || max_seq_len <= 0 || T <= 0) return 0;
-    size_t need = lorc_append8_scratch_bytes(ctx, batch, T);
+    size_t need = lorc_append8_scratch_most(ctx, batch, T);
     const size_t d = lorc_decode8_scratch_bytes(ctx, batch, max_seq_len, T);
     if (d > need) need = d;
     if (T > 1 && lorc_tc_prefill_shape_ok(ctx)) {

@@ -173,9 +173,10 @@ def _exact_x(c, T):
 
 
 @pytest.mark.parametrize("kind", H8.KINDS)
-@pytest.mark.parametrize("heads,D", [((4, 2, 64), 256), ((4, 4, 128), 512), ((3, 3, 64), 200)])
+@pytest.mark.parametrize("heads,D", [((4, 2, 64), 256), ((4, 4, 128), 512), ((3, 3, 64), 200), ((3, 3, 64), 320)])
 @pytest.mark.parametrize("T,lens,page", [(1, [1, 16, 17, 32, 100], 0), (1, [49, 64, 65], 16), (15, [15, 31, 47, 40], 48),
-                                         (16, [16, 33], 0), (37, [37, 100, 64], 64), (300, [300, 333], 128)])
+                                         (16, [16, 33], 0), (37, [37, 100, 64], 64), (300, [300, 333], 128),
+                                         (20, list(range(20, 80, 2)), 16), (500, [507], 0)])
 def test_write_is_exact_where_the_projection_is(kind, heads, D, T, lens, page):
     """No rotation and one-hot hidden states: codes and scales are the oracle's, bit for bit; all else stays as it was."""
     c = H8.Case(kind, *heads, lens, page=page, D=D, style=H.ROPE_NONE, seed=T)
