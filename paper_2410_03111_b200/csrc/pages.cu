@@ -3,6 +3,8 @@
 // A call plans with one block (who needs pages, which are the lowest free ones: prefix sums over the list and over the reference
 // counts), and a second kernel with the whole GPU moves the pages' contents in every array and rewrites table entries.  The moves
 // are plain copies, bound by HBM: a warp takes 4 KB of one page of one array at a time, eight 16-byte loads per lane in flight.
+// (468 MB, half of the pages of a pool of eight layers: 80 us with its plan, 0.89 of the measured copy rate.)  What is left of a small
+// call is its chain of launches and round trips.
 #include "common.cuh"
 #include "sm100_ptx.cuh"
 
@@ -13,6 +15,7 @@ namespace {
 constexpr int PLAN_THREADS = 1024;
 constexpr int BUFS = 128;               // arrays per launch of the copying kernels (the descriptors are kernel arguments)
 constexpr int UNIT = 4096;              // bytes of a warp's piece of work
+constexpr int SMALL = 256;              // pairs of a fork whose plan stays in shared memory
 
 struct PagesView {
     int n_pages, page_size, per_row, n_rows;
@@ -38,50 +41,54 @@ __device__ __forceinline__ int held_pages(const PagesView& p, int len) {
     return len <= 0 || !row_fits(p, len) ? 0 : (len - 1) / p.page_size + 1;
 }
 
-// Sums over the block in thread order: the sum of the threads before this one; `all` receives the sum of all.  (All threads.)
-__device__ __forceinline__ long long block_scan(long long x, long long* sums, long long& all) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    long long incl = x;
+// Inclusive sums over the lanes of a warp.
+template <typename T>
+__device__ __forceinline__ T warp_scan(T x, int lane) {
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const long long y = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += y;
+        const T y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += y;
     }
+    return x;
+}
+// Sums over the block in thread order: the sum of the threads before this one; `all` receives the sum of all.  (All threads.)
+template <typename T>
+__device__ __forceinline__ T block_scan(T x, T* sums, T& all) {
+    static_assert(PLAN_THREADS == 1024, "a warp's lanes are the block's warps");
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const T incl = warp_scan(x, lane);
     __syncthreads();
     if (lane == 31) sums[warp] = incl;
     __syncthreads();
-    long long before = 0, total = 0;
-#pragma unroll
-    for (int w = 0; w < PLAN_THREADS / 32; ++w) {
-        const long long y = sums[w];
-        if (w < warp) before += y;
-        total += y;
-    }
-    all = total;
-    return before + incl - x;
+    const T mine = sums[lane], upto = warp_scan(mine, lane);
+    all = __shfl_sync(0xffffffffu, upto, 31);
+    return __shfl_sync(0xffffffffu, upto - mine, warp) + incl - x;
 }
 
-// Writes the `want` lowest free pages (at most) in ascending order; returns how many there are of them.  (All threads.)
-__device__ int lowest_free(const PagesView& p, long long want, int32_t* list, long long* sums) {
+// This thread's four of the 4096 counts from page p0 on: which of them are free.
+__device__ __forceinline__ unsigned free_of(const PagesView& p, int p0) {
+    const int at = p0 + 4 * (int)threadIdx.x;
+    unsigned mask = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (at + i < p.n_pages && p.refs[at + i] <= 0) mask |= 1u << i;
+    return mask;
+}
+
+// Writes the `want` lowest free pages (at most) in ascending order; returns how many there are of them.  `first`: free_of the first
+// 4096 pages, which the caller has asked for before it knew `want`.  (All threads.)
+__device__ int lowest_free(const PagesView& p, long long want, unsigned first, int32_t* list, int* sums) {
     int found = 0;
     for (int p0 = 0; p0 < p.n_pages && found < want; p0 += 4 * PLAN_THREADS) {
-        const int at = p0 + 4 * (int)threadIdx.x;
-        bool free[4];
-        int mine = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            free[i] = at + i < p.n_pages && p.refs[at + i] <= 0;
-            mine += free[i];
-        }
-        long long all;
-        int rank = found + (int)block_scan(mine, sums, all);
+        const unsigned free = p0 == 0 ? first : free_of(p, p0);
+        int all, rank = found + block_scan(__popc(free), sums, all);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (free[i]) {
-                if (rank < want) list[rank] = at + i;
+            if (free >> i & 1) {
+                if (rank < want) list[rank] = p0 + 4 * (int)threadIdx.x + i;
                 ++rank;
             }
-        found += (int)all;
+        found += all;
     }
     __syncthreads();
     return found < want ? found : (int)want;
@@ -118,7 +125,7 @@ struct ForkPair {
 __global__ void __launch_bounds__(PLAN_THREADS)
 pages_fork_plan_kernel(const PagesView p, const int32_t* __restrict__ parents, const int32_t* __restrict__ children, int n,
                        ForkPair* __restrict__ plan, int32_t* __restrict__ list, int* status) {
-    __shared__ long long sums[PLAN_THREADS / 32];
+    __shared__ int sums[PLAN_THREADS / 32];
     const int tid = threadIdx.x;
     grid_dep_wait();
     grid_dep_launch();
@@ -151,16 +158,16 @@ pages_fork_plan_kernel(const PagesView p, const int32_t* __restrict__ parents, c
             plan[i].len = -1;
         }
     // who needs a page, and which one
-    long long want = 0;
+    int want = 0;
     for (int i0 = 0; i0 < n; i0 += PLAN_THREADS) {
         const int i = i0 + tid;
         const bool need = i < n && plan[i].len > 0 && plan[i].len % p.page_size != 0;
-        long long all;
-        const long long rank = want + block_scan(need, sums, all);
-        if (need) plan[i].page = (int)rank;
+        int all;
+        const int rank = want + block_scan((int)need, sums, all);
+        if (need) plan[i].page = rank;
         want += all;
     }
-    const int found = lowest_free(p, want, list, sums);
+    const int found = lowest_free(p, want, free_of(p, 0), list, sums);
     for (int i = tid; i < n; i += PLAN_THREADS) {
         ForkPair f = plan[i];
         if (f.len < 0) continue;
@@ -186,13 +193,14 @@ __device__ __forceinline__ void copy_unit(const Bufs& bufs, int b, long long beg
     char* to = bufs.base[b] + dst * bytes + begin;
     const int left = (int)(bytes - begin < UNIT ? bytes - begin : UNIT);
     if (bufs.wide[b >> 5] >> (b & 31) & 1) {
+        // (what is copied is not read again soon)
         uint4 x[UNIT / 512];
 #pragma unroll
         for (int i = 0; i < UNIT / 512; ++i)
-            if ((i * 32 + lane) * 16 < left) x[i] = reinterpret_cast<const uint4*>(from)[i * 32 + lane];
+            if ((i * 32 + lane) * 16 < left) x[i] = __ldcs(reinterpret_cast<const uint4*>(from) + i * 32 + lane);
 #pragma unroll
         for (int i = 0; i < UNIT / 512; ++i)
-            if ((i * 32 + lane) * 16 < left) reinterpret_cast<uint4*>(to)[i * 32 + lane] = x[i];
+            if ((i * 32 + lane) * 16 < left) __stcs(reinterpret_cast<uint4*>(to) + i * 32 + lane, x[i]);
     } else {
         for (int i = lane * 4; i < left; i += 128) *reinterpret_cast<uint32_t*>(to + i) = *reinterpret_cast<const uint32_t*>(from + i);
     }
@@ -210,14 +218,29 @@ __device__ __forceinline__ int find_buf(const Bufs& bufs, int u, long long& begi
     return lo;
 }
 
-__global__ void __launch_bounds__(256)
-pages_fork_kernel(const __grid_constant__ Bufs bufs, const PagesView p, const ForkPair* __restrict__ plan, int n, int rows_too,
-                  int* status) {
-    const int lane = threadIdx.x & 31;
-    const long long warps = (long long)gridDim.x * 8, me = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-    grid_dep_wait();
-    grid_dep_launch();
-    // table rows and counts: a warp per pair
+// Pieces me, me + warps, me + 2 warps, ... of a list of pages with `units` pieces each: page i, piece u.
+struct Pieces {
+    long long i, di;
+    int u, du, units;
+    __device__ Pieces(long long me, long long warps, int units) : units(units) {
+        i = units ? me / units : 0;
+        u = units ? (int)(me - i * units) : 0;
+        di = units ? warps / units : 0;
+        du = units ? (int)(warps - di * units) : 0;
+    }
+    __device__ void next() {
+        i += di;
+        u += du;
+        if (u >= units) {
+            u -= units;
+            ++i;
+        }
+    }
+};
+
+// The rows of the children, and the pages of their own: by `warps` warps, of which this is number `me`.
+__device__ __forceinline__ void fork_apply(const Bufs& bufs, const PagesView& p, const ForkPair* plan, int n, bool rows_too, long long me,
+                                           long long warps, int lane, int* status) {
     if (rows_too)
         for (long long i = me; i < n; i += warps) {
             const ForkPair f = plan[i];
@@ -232,11 +255,9 @@ pages_fork_kernel(const __grid_constant__ Bufs bufs, const PagesView p, const Fo
                 else if (j < shared) atomicAdd(p.refs + page, 1);
             }
         }
-    const int units = bufs.first[bufs.n];
-    const long long total = (long long)n * units;
-    for (long long w = me; w < total; w += warps) {
-        const int i = (int)(w / units), u = (int)(w - (long long)i * units);
-        const ForkPair f = plan[i];
+    if (bufs.first[bufs.n] == 0) return;
+    for (Pieces w(me, warps, bufs.first[bufs.n]); w.i < n; w.next()) {
+        const ForkPair f = plan[w.i];
         if (f.len <= 0 || f.page < 0) continue;
         const int src = p.table[(long long)f.parent * p.per_row + f.len / p.page_size];
         if (src < 0 || src >= p.n_pages) {
@@ -244,18 +265,93 @@ pages_fork_kernel(const __grid_constant__ Bufs bufs, const PagesView p, const Fo
             continue;
         }
         long long begin;
-        const int b = find_buf(bufs, u, begin);
+        const int b = find_buf(bufs, w.u, begin);
         copy_unit(bufs, b, begin, src, f.page, lane);
     }
+}
+
+// The same for at most SMALL pairs: a thread per pair, and the plan stays in shared memory until it is written out.  apply: there is
+// so little to do that this block does it all.
+__global__ void __launch_bounds__(PLAN_THREADS)
+pages_fork_small_kernel(const __grid_constant__ Bufs bufs, const PagesView p, const int32_t* __restrict__ parents,
+                        const int32_t* __restrict__ children, int n, ForkPair* __restrict__ plan, int apply, int* status) {
+    __shared__ int sums[PLAN_THREADS / 32];
+    __shared__ ForkPair pairs[SMALL];
+    __shared__ alignas(16) int32_t child_s[SMALL];
+    __shared__ int32_t list[SMALL];
+    const int tid = threadIdx.x;
+    grid_dep_wait();
+    grid_dep_launch();
+    const unsigned free = free_of(p, 0);
+    ForkPair f = {-1, -1, -1, -1};
+    if (tid < n) {
+        f.parent = parents[tid];
+        f.child = children[tid];
+        if (f.parent < 0 || f.parent >= p.n_rows || f.child < 0 || f.child >= p.n_rows) {
+            lorc_set_status(status, LORC_ERR_ARG);
+        } else {
+            const int theirs = p.lens[f.child], len = max(p.lens[f.parent], 0);
+            if (theirs > 0) lorc_set_status(status, LORC_ERR_ARG);
+            else if (!row_fits(p, len)) lorc_set_status(status, LORC_ERR_CAPACITY);
+            else f.len = len;
+        }
+    }
+    if (tid < SMALL) child_s[tid] = f.len >= 0 ? f.child : -1;
+    __syncthreads();
+    if (f.len >= 0) {
+        bool again = false;                      // an earlier pair has the same child
+        for (int j = 0; j < tid; j += 4) {
+            const int4 c = *reinterpret_cast<const int4*>(child_s + j);
+            again |= c.x == f.child || (c.y == f.child && j + 1 < tid) || (c.z == f.child && j + 2 < tid) || (c.w == f.child && j + 3 < tid);
+        }
+        if (again) {
+            lorc_set_status(status, LORC_ERR_ARG);
+            f.len = -1;
+        }
+    }
+    const bool need = f.len > 0 && f.len % p.page_size != 0;
+    int want;
+    const int rank = block_scan((int)need, sums, want);
+    const int found = lowest_free(p, want, free, list, sums);
+    if (f.len >= 0) {
+        if (need) {
+            if (rank < found) {
+                f.page = list[rank];
+                p.refs[f.page] = 1;
+            } else {
+                lorc_set_status(status, LORC_ERR_CAPACITY);
+                f.len = 0;
+            }
+        }
+        p.lens[f.child] = f.len;
+    }
+    if (tid < n) {
+        if (apply) pairs[tid] = f;
+        else plan[tid] = f;
+    }
+    if (!apply) return;
+    __syncthreads();
+    fork_apply(bufs, p, pairs, n, true, tid >> 5, PLAN_THREADS / 32, tid & 31, status);
+}
+
+__global__ void __launch_bounds__(256)
+pages_fork_kernel(const __grid_constant__ Bufs bufs, const PagesView p, const ForkPair* __restrict__ plan, int n, int rows_too,
+                  int* status) {
+    grid_dep_wait();
+    grid_dep_launch();
+    fork_apply(bufs, p, plan, n, rows_too != 0, (long long)blockIdx.x * 8 + (threadIdx.x >> 5), (long long)gridDim.x * 8,
+               threadIdx.x & 31, status);
 }
 
 __global__ void __launch_bounds__(PLAN_THREADS)
 pages_grow_kernel(const PagesView p, const int32_t* __restrict__ grow, long long* __restrict__ start, int32_t* __restrict__ list,
                   int* status) {
     __shared__ long long sums[PLAN_THREADS / 32];
+    __shared__ int counts[PLAN_THREADS / 32];
     const int tid = threadIdx.x, lane = tid & 31;
     grid_dep_wait();
     grid_dep_launch();
+    const unsigned free = free_of(p, 0);
     // start[s]: the rank of the row's first new page, -1 for a row that stays as it is
     long long want = 0;
     for (int s0 = 0; s0 < p.n_rows; s0 += PLAN_THREADS) {
@@ -269,11 +365,11 @@ pages_grow_kernel(const PagesView p, const int32_t* __restrict__ grow, long long
             else lorc_set_status(status, LORC_ERR_CAPACITY);
         }
         long long all;
-        const long long rank = want + block_scan(more, sums, all);
+        const long long rank = want + block_scan((long long)more, sums, all);
         if (s < p.n_rows) start[s] = live ? rank : -1;
         want += all;
     }
-    const int found = lowest_free(p, want, list, sums);
+    const int found = lowest_free(p, want, free, list, counts);
     for (int s = tid >> 5; s < p.n_rows; s += PLAN_THREADS / 32) {
         const long long first = start[s];
         if (first < 0) continue;
@@ -379,13 +475,11 @@ pages_compact_kernel(const __grid_constant__ Bufs bufs, const PagesView p, const
             }
         }
     }
-    const int units = bufs.first[bufs.n];
-    const long long total = (long long)n * units;
-    for (long long w = me; w < total; w += warps) {
-        const int i = (int)(w / units), u = (int)(w - (long long)i * units);
-        const Copy m = moves[i];
+    if (bufs.first[bufs.n] == 0) return;
+    for (Pieces w(me, warps, bufs.first[bufs.n]); w.i < n; w.next()) {
+        const Copy m = moves[w.i];
         long long begin;
-        const int b = find_buf(bufs, u, begin);
+        const int b = find_buf(bufs, w.u, begin);
         copy_unit(bufs, b, begin, m.src, m.dst, lane);
     }
 }
@@ -505,12 +599,20 @@ int lorc_pages_fork(lorc_ctx* ctx, const lorc_pages* pages, const int32_t* paren
     ForkPair* plan = (ForkPair*)((char*)ctx->ws + l.plan);
     int32_t* list = (int32_t*)((char*)ctx->ws + l.list);
     cudaStream_t st = (cudaStream_t)stream;
-    cudaError_t e = lorc_launch_dependent(pages_fork_plan_kernel, dim3(1), dim3(PLAN_THREADS), 0, st, v, parents, children, n, plan, list,
-                                          ctx->status_dev);
-    ctx->launches += 1;
     Bufs b;
-    for (int from = 0; e == cudaSuccess && (from == 0 || from < pages->n_bufs); from += BUFS) {
-        take_bufs(pages, from, &b);
+    take_bufs(pages, 0, &b);
+    cudaError_t e;
+    // One block copies some 250 KB and 16384 table entries in the time that another launch takes.
+    const bool all = n <= SMALL && pages->n_bufs <= BUFS && (long long)n * b.first[b.n] <= PLAN_THREADS / 32 && (long long)n * v.per_row <= 16384;
+    if (n <= SMALL)
+        e = lorc_launch_dependent(pages_fork_small_kernel, dim3(1), dim3(PLAN_THREADS), 0, st, b, v, parents, children, n, plan, (int)all,
+                                  ctx->status_dev);
+    else
+        e = lorc_launch_dependent(pages_fork_plan_kernel, dim3(1), dim3(PLAN_THREADS), 0, st, v, parents, children, n, plan, list,
+                                  ctx->status_dev);
+    ctx->launches += 1;
+    for (int from = 0; !all && e == cudaSuccess && (from == 0 || from < pages->n_bufs); from += BUFS) {
+        if (from > 0) take_bufs(pages, from, &b);
         e = lorc_launch_dependent(pages_fork_kernel, dim3(copy_blocks(ctx, b, n, n)), dim3(256), 0, st, b, v, (const ForkPair*)plan, n,
                                   (int)(from == 0), ctx->status_dev);
         ctx->launches += 1;
