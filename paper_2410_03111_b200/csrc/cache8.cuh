@@ -105,8 +105,10 @@ size_t lorc_decode8_scratch_bytes(const lorc_ctx* ctx, int batch, int max_seq_le
 cudaError_t lorc_decode8_launch(lorc_ctx* ctx, const Cache8View& cv, const bf16* q, bf16* out, int T, void* scratch,
                                 cudaStream_t st, int* launches);
 
-// Attention of prompt chunks on tcgen05 (prefill8.cu).
-bool lorc_prefill8_supported(const lorc_ctx* ctx);
-size_t lorc_prefill8_scratch_bytes(const lorc_ctx* ctx, int batch, int max_seq_len);
+// Attention of prompt chunks on tcgen05 (prefill8.cu).  Scratch of a call, and of any call with at most as many sequences, tokens and
+// queries.
+bool lorc_prefill8_supported(const lorc_ctx* ctx, const Cache8View& cv, int T);
+size_t lorc_prefill8_scratch_bytes(const lorc_ctx* ctx, int batch, int max_seq_len, int T);
+size_t lorc_prefill8_scratch_most(const lorc_ctx* ctx, int batch, int max_seq_len, int T);
 cudaError_t lorc_prefill8_launch(lorc_ctx* ctx, const Cache8View& cv, const bf16* q, bf16* out, int T, void* scratch,
                                  cudaStream_t st, int* launches);

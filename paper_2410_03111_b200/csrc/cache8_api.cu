@@ -72,9 +72,9 @@ int attend8(lorc_ctx* ctx, int layer, const lorc_cache8* cache, const void* q, v
     Cache8View cv;
     const int rc = check8(ctx, layer, cache, T, q, out, &cv);
     if (rc) return rc;
-    const bool expand = T > 1 && cv.batch <= 65535 && lorc_prefill8_supported(ctx);
+    const bool expand = lorc_prefill8_supported(ctx, cv, T);
     if (!lorc_get_tmap_encode()) return fail8(ctx, LORC_ERR_CUDA, "cache8: the driver offers no tensor maps");
-    const size_t need = expand ? lorc_prefill8_scratch_bytes(ctx, cv.batch, cv.max_seq_len)
+    const size_t need = expand ? lorc_prefill8_scratch_bytes(ctx, cv.batch, cv.max_seq_len, T)
                                : lorc_decode8_scratch_bytes(ctx, cv.batch, cv.max_seq_len, T);
     if (!ctx->ws || need > ctx->ws_bytes)
         return fail8(ctx, LORC_ERR_WORKSPACE, "cache8: workspace missing or too small (see lorc_cache8_workspace_bytes)");
@@ -101,7 +101,7 @@ size_t lorc_cache8_workspace_bytes(const lorc_ctx* ctx, int batch, int max_seq_l
     const size_t d = lorc_decode8_scratch_bytes(ctx, batch, max_seq_len, T);
     if (d > need) need = d;
     if (T > 1 && lorc_tc_prefill_shape_ok(ctx)) {
-        const size_t f = lorc_prefill8_scratch_bytes(ctx, batch, max_seq_len);
+        const size_t f = lorc_prefill8_scratch_most(ctx, batch, max_seq_len, T);
         if (f > need) need = f;
     }
     return need;

@@ -1,7 +1,7 @@
 // Prompt chunks over the 8-bit cache of uncompressed layers: keys and values of the cached tokens are brought to fp16 once per
 // call (code x scale: seven significant bits, exact unless the scale is no power of two), then the tcgen05 attention kernel of the
 // latent mode runs over them.  With T queries per sequence that kernel does 4 T d G products per number of the buffer, so the
-// pass over it is small for chunks; a call with few queries is better served by the streaming kernel.
+// pass over it is small for chunks.
 #include <math.h>
 
 #include "cache8.cuh"
@@ -70,14 +70,53 @@ expand8_kernel(const Expand8Params p) {
 
 size_t expand8_rows(int max_seq_len) { return ((size_t)max_seq_len + 127) / 128 * 128; }
 
-}  // namespace
+constexpr int MAX_SPLIT = 16;
 
-bool lorc_prefill8_supported(const lorc_ctx* ctx) {
-    return lorc_tc_prefill_shape_ok(ctx) && !(ctx->desc.flags & LORC_FLAG_DEBUG_FP32) && lorc_get_tmap_encode() != nullptr;
+// Time of the attention kernel (and its merge) in tenths of a microsecond with the keys of a block of query rows shared by S CTAs: a
+// CTA takes 2.2 us per tile of 128 keys and 4 us before and after, whatever runs beside it; the merge 3 us and its traffic.
+long long attend8_time(const lorc_ctx* ctx, long long blocks, long long tiles, int S) {
+    const long long waves = (blocks * S + ctx->sm_count - 1) / ctx->sm_count;
+    return waves * ((tiles + S - 1) / S * 22 + 40) + (S > 1 ? 30 + blocks * S * 256 * 130 * 8 / 500000 : 0);
 }
 
-size_t lorc_prefill8_scratch_bytes(const lorc_ctx* ctx, int batch, int max_seq_len) {
+// CTAs per pair of blocks of query rows: as many as pay.  (One prompt chunk of 256 tokens behind 8000: 152 us with one, 41 with four.)
+int prefill8_split(const lorc_ctx* ctx, int batch, int max_seq_len, int T) {
+    const int qp = 256 / ctx->group;
+    const long long blocks = (long long)batch * ctx->desc.n_kv_heads * ((T + qp - 1) / qp), tiles = ((long long)max_seq_len + 127) / 128;
+    int best = 1;
+    for (int S = 2; S <= MAX_SPLIT && 2 * S <= tiles && blocks * S <= 2ll * ctx->sm_count; ++S)
+        if (attend8_time(ctx, blocks, tiles, S) < attend8_time(ctx, blocks, tiles, best)) best = S;
+    return best;
+}
+
+size_t expand8_bytes(const lorc_ctx* ctx, int batch, int max_seq_len) {
     return 2 * lorc_align_up((size_t)batch * expand8_rows(max_seq_len) * ctx->n * 2, 256);
+}
+
+}  // namespace
+
+// Few queries per sequence are better served by the streaming kernel, which reads the codes once per query (from L2, mostly) and is
+// then bound by its arithmetic: 0.33 us per 64 tokens, query and KV head on an SM, against 1.3 us to expand them for all queries (8 x 4096
+// tokens, 8B shape, 4 queries 43 us against 112, 16 queries 147 against 108; one sequence of 1000 tokens, 32 queries 16 against 26).
+bool lorc_prefill8_supported(const lorc_ctx* ctx, const Cache8View& cv, int T) {
+    if (T == 1 || cv.batch > 65535 || !lorc_tc_prefill_shape_ok(ctx) || (ctx->desc.flags & LORC_FLAG_DEBUG_FP32)) return false;
+    const int qp = 256 / ctx->group;
+    const long long blocks = (long long)cv.batch * cv.n_kv * ((T + qp - 1) / qp), tiles = ((long long)cv.max_seq_len + 127) / 128;
+    const long long units = (long long)cv.batch * cv.n_kv * ((cv.max_seq_len + 63) / 64), P = ctx->sm_count;
+    const long long stream = 80 + 33 * units * T / (10 * P);
+    const long long expand = 100 + 13 * units / P + attend8_time(ctx, blocks, tiles, prefill8_split(ctx, cv.batch, cv.max_seq_len, T));
+    return expand < stream;
+}
+
+size_t lorc_prefill8_scratch_bytes(const lorc_ctx* ctx, int batch, int max_seq_len, int T) {
+    return expand8_bytes(ctx, batch, max_seq_len) +
+           lorc_tc_prefill_part_bytes(ctx, batch, T, prefill8_split(ctx, batch, max_seq_len, T));
+}
+
+size_t lorc_prefill8_scratch_most(const lorc_ctx* ctx, int batch, int max_seq_len, int T) {
+    // a call with fewer tokens may share their keys among more CTAs: at most MAX_SPLIT, and two blocks of 256 rows per SM
+    const size_t rows = (size_t)batch * T * ctx->desc.n_q_heads * MAX_SPLIT, cap = 2 * (size_t)ctx->sm_count * 256;
+    return expand8_bytes(ctx, batch, max_seq_len) + (rows < cap ? rows : cap) * 130 * sizeof(float);
 }
 
 cudaError_t lorc_prefill8_launch(lorc_ctx* ctx, const Cache8View& cv, const bf16* q, bf16* out, int T, void* scratch,
@@ -94,12 +133,14 @@ cudaError_t lorc_prefill8_launch(lorc_ctx* ctx, const Cache8View& cv, const bf16
     Expand8Params p;
     p.cv = cv; p.status = ctx->status_dev; p.rows = (long long)rows; p.max_pos = ctx->desc.max_pos; p.T = T;
     p.khat = (uint4*)scratch;
-    p.vbuf = (uint4*)((char*)scratch + lorc_prefill8_scratch_bytes(ctx, cv.batch, cv.max_seq_len) / 2);
+    const size_t kv = expand8_bytes(ctx, cv.batch, cv.max_seq_len);
+    p.vbuf = (uint4*)((char*)scratch + kv / 2);
     p.dh_shift = ctx->desc.d_head == 128 ? 7 : 6;
     const dim3 grid((unsigned)(rows / LORC_BLOCK8), (unsigned)cv.batch, 2);
     e = cv.type == LORC_CACHE8_E4M3 ? lorc_launch_dependent(expand8_kernel<true>, grid, dim3(256), 0, st, p)
                                     : lorc_launch_dependent(expand8_kernel<false>, grid, dim3(256), 0, st, p);
     *launches += 1;
     if (e != cudaSuccess) return e;
-    return lorc_tc_prefill_attend(ctx, cv.seq_lens, cv.batch, rows, cv.max_seq_len, p.khat, p.vbuf, q, out, T, st, launches);
+    return lorc_tc_prefill_attend(ctx, cv.seq_lens, cv.batch, rows, cv.max_seq_len, p.khat, p.vbuf, q, out, T,
+                                  prefill8_split(ctx, cv.batch, cv.max_seq_len, T), (float*)((char*)scratch + kv), st, launches);
 }

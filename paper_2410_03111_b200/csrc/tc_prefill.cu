@@ -337,6 +337,9 @@ struct FaParams {
     const float2* rope_table;      // [max_pos][64]
     int* status;
     int T, H_q, G, n_rows, max_pos;
+    int n_split;                   // SPLIT: CTAs that share the keys of two blocks of query rows
+    float* part_ml;                // SPLIT: [n_split][b, T, H_q][2] reference, sum of the row's probabilities
+    float* part_o;                 // SPLIT: [n_split][b, T, H_q][128] un-normalised output
 };
 
 __device__ __forceinline__ float ex2_approx(float x) {
@@ -361,6 +364,9 @@ __device__ __forceinline__ void probs_chunk(const uint32_t (&r)[32], float m, ui
     tmem_st16(taddr, w);
 }
 
+// SPLIT: n_split CTAs share the key tiles of the two blocks of query rows (where there are fewer blocks than SMs), in contiguous
+// equal parts; each leaves its rows' references, sums and un-normalised outputs for a merge kernel.
+template <bool SPLIT>
 __global__ void __launch_bounds__(F_THREADS, 1)
 lorc_prefill_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUtensorMap mapK,
                          const __grid_constant__ CUtensorMap mapV, const FaParams p) {
@@ -370,7 +376,9 @@ lorc_prefill_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_
     const int g = blockIdx.y, s = blockIdx.z;
     const int qp = TILE / p.G;                                // query positions per block of 128 rows
     // the CTAs with the latest positions see the most keys: they go first
-    const int t0 = ((int)gridDim.x - 1 - (int)blockIdx.x) * 2 * qp;   // first position (inside the chunk) of this CTA
+    const int bx = SPLIT ? (int)blockIdx.x / p.n_split : (int)blockIdx.x, nx = SPLIT ? (int)gridDim.x / p.n_split : (int)gridDim.x;
+    const int part = SPLIT ? (int)blockIdx.x - bx * p.n_split : 0;
+    const int t0 = (nx - 1 - bx) * 2 * qp;                    // first position (inside the chunk) of this CTA
     if (tid == 0) {
         mbar_init(&sm.q_full, 1);
         mbar_init(&sm.q_ready, 8);
@@ -402,7 +410,12 @@ lorc_prefill_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_
         len = 0;
     }
     const int t_last = min(p.T, t0 + 2 * qp) - 1;             // last query position of the CTA
-    const int n_tiles = len > 0 ? (len - p.T + t_last) / TILE + 1 : 0;
+    int n_tiles = len > 0 ? (len - p.T + t_last) / TILE + 1 : 0, j_first = 0;
+    if (SPLIT) {                                              // this CTA's tiles: n_tiles of them from j_first on
+        const int per = (n_tiles + p.n_split - 1) / p.n_split;
+        j_first = part * per;
+        n_tiles = max(0, min(n_tiles - j_first, per));
+    }
 
     if (warp == 1) {
         tmem_alloc(&sm.tmem_base, 512);
@@ -433,15 +446,15 @@ lorc_prefill_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_
                 if (!mbar_wait(&sm.k_empty[st], par)) { ok = false; break; }
                 if (elect_one()) {
                     mbar_arrive_expect_tx(&sm.k_full[st], 2 * TILE * KC * 2);
-                    tma_load_3d(sm.K[st][0], &mapK, &sm.k_full[st], g * 128, j * TILE, s);
-                    tma_load_3d(sm.K[st][1], &mapK, &sm.k_full[st], g * 128 + 64, j * TILE, s);
+                    tma_load_3d(sm.K[st][0], &mapK, &sm.k_full[st], g * 128, (j_first + j) * TILE, s);
+                    tma_load_3d(sm.K[st][1], &mapK, &sm.k_full[st], g * 128 + 64, (j_first + j) * TILE, s);
                 }
                 __syncwarp();
                 if (!mbar_wait(&sm.v_empty[st], par)) { ok = false; break; }
                 if (elect_one()) {
                     mbar_arrive_expect_tx(&sm.v_full[st], 2 * TILE * KC * 2);
-                    tma_load_3d(sm.V[st][0], &mapV, &sm.v_full[st], g * 128, j * TILE, s);
-                    tma_load_3d(sm.V[st][1], &mapV, &sm.v_full[st], g * 128 + 64, j * TILE, s);
+                    tma_load_3d(sm.V[st][0], &mapV, &sm.v_full[st], g * 128, (j_first + j) * TILE, s);
+                    tma_load_3d(sm.V[st][1], &mapV, &sm.v_full[st], g * 128 + 64, (j_first + j) * TILE, s);
                 }
                 __syncwarp();
             }
@@ -562,7 +575,7 @@ lorc_prefill_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_
         for (int j = 0; j < n_tiles && ok; ++j) {
             if (!mbar_wait(&sm.s_full[b], j & 1)) { ok = false; break; }
             tc_fence_after_sync();
-            const int n0 = j * TILE;
+            const int n0 = (j_first + j) * TILE;
             // the whole row of scores in registers
             uint32_t r0[32], r1[32], r2[32], r3[32];
             tmem_ld32(trow, r0);
@@ -633,31 +646,48 @@ lorc_prefill_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_
             tc_fence_after_sync();
             const bool has_out = t0 + tt < p.T;                // (rows past the chunk still take part in the warp-wide loads)
             const float l = l0 + l1;
-            const float inv = l > 0.f ? 1.f / l : 0.f;
-            // a NaN means non-finite numbers in the cache, the factors or the query (or a key beyond the fp16 range)
-            if (has_out && l != l) lorc_set_status(p.status, LORC_ERR_ARG);
-            if (has_out && !(l > 0.f) && l == l && hi == 0 && g == 0 && t0 + tt == 0) lorc_set_status(p.status, LORC_ERR_EMPTY);
-            bf16* dst = p.out + (((long long)s * p.T + (has_out ? t0 + tt : 0)) * p.H_q + g * p.G + hi) * 128;
-#pragma unroll
-            for (int c0 = 0; c0 < TILE; c0 += 32) {
-                uint32_t o[32];
+            if (SPLIT) {
+                const long long at = (((long long)part * gridDim.z + s) * p.T + (has_out ? t0 + tt : 0)) * p.H_q + g * p.G + hi;
+                if (has_out) *reinterpret_cast<float2*>(p.part_ml + at * 2) = make_float2(m_ref, l);
                 if (n_tiles > 0) {
-                    tmem_ld32(orow + c0, o);
-                    tmem_wait_ld();
-                } else {
+#pragma unroll 1
+                    for (int c0 = 0; c0 < TILE; c0 += 16) {
+                        uint32_t o[16];
+                        tmem_ld16(orow + c0, o);
+                        tmem_wait_ld();
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) o[i] = 0u;
-                }
-#pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    uint32_t w[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const __nv_bfloat162 b2 = __floats2bfloat162_rn(__uint_as_float(o[v * 8 + 2 * e]) * inv,
-                                                                        __uint_as_float(o[v * 8 + 2 * e + 1]) * inv);
-                        w[e] = *reinterpret_cast<const uint32_t*>(&b2);
+                        for (int v = 0; v < 4; ++v)
+                            if (has_out)
+                                reinterpret_cast<uint4*>(p.part_o + at * 128 + c0)[v] = make_uint4(o[4 * v], o[4 * v + 1], o[4 * v + 2], o[4 * v + 3]);
                     }
-                    if (has_out) reinterpret_cast<uint4*>(dst + c0)[v] = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+            } else {
+                const float inv = l > 0.f ? 1.f / l : 0.f;
+                // a NaN means non-finite numbers in the cache, the factors or the query (or a key beyond the fp16 range)
+                if (has_out && l != l) lorc_set_status(p.status, LORC_ERR_ARG);
+                if (has_out && !(l > 0.f) && l == l && hi == 0 && g == 0 && t0 + tt == 0) lorc_set_status(p.status, LORC_ERR_EMPTY);
+                bf16* dst = p.out + (((long long)s * p.T + (has_out ? t0 + tt : 0)) * p.H_q + g * p.G + hi) * 128;
+    #pragma unroll
+                for (int c0 = 0; c0 < TILE; c0 += 32) {
+                    uint32_t o[32];
+                    if (n_tiles > 0) {
+                        tmem_ld32(orow + c0, o);
+                        tmem_wait_ld();
+                    } else {
+    #pragma unroll
+                        for (int i = 0; i < 32; ++i) o[i] = 0u;
+                    }
+    #pragma unroll
+                    for (int v = 0; v < 4; ++v) {
+                        uint32_t w[4];
+    #pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const __nv_bfloat162 b2 = __floats2bfloat162_rn(__uint_as_float(o[v * 8 + 2 * e]) * inv,
+                                                                            __uint_as_float(o[v * 8 + 2 * e + 1]) * inv);
+                            w[e] = *reinterpret_cast<const uint32_t*>(&b2);
+                        }
+                        if (has_out) reinterpret_cast<uint4*>(dst + c0)[v] = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
                 }
             }
         }
@@ -666,6 +696,59 @@ lorc_prefill_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_
     tc_fence_before_sync();
     __syncthreads();
     if (warp == 1) tmem_dealloc(tmem, 512);
+}
+
+// Merge of the parts of a row (b, t, head): one warp per row, four dimensions per lane.
+__global__ void __launch_bounds__(256)
+lorc_prefill_merge_kernel(const float* __restrict__ part_ml, const float* __restrict__ part_o, bf16* __restrict__ out, int n_split,
+                          long long rows, int T, int H_q, int* status) {
+    const int lane = threadIdx.x & 31;
+    const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+    grid_dep_wait();
+    grid_dep_launch();
+    if (row >= rows) return;
+    float M = -INFINITY, L = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int c0 = 0; c0 < n_split; c0 += 4) {
+        float2 ml[4];
+        float4 o[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            ml[c] = make_float2(0.f, 0.f);
+            o[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (c0 + c < n_split) {
+                ml[c] = *reinterpret_cast<const float2*>(part_ml + ((c0 + c) * rows + row) * 2);
+                // (a part without tokens has left no output)
+                if (ml[c].y != 0.f) o[c] = *reinterpret_cast<const float4*>(part_o + ((c0 + c) * rows + row) * 128 + lane * 4);
+            }
+        }
+        float now = M;
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            if (ml[c].y != 0.f) now = fmaxf(now, ml[c].x);
+        if (now > M) {
+            const float alpha = M == -INFINITY ? 0.f : exp2f(M - now);
+            L *= alpha;
+            acc.x *= alpha; acc.y *= alpha; acc.z *= alpha; acc.w *= alpha;
+            M = now;
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            if (ml[c].y == 0.f) continue;
+            const float w = exp2f(ml[c].x - M);
+            L += w * ml[c].y;
+            acc.x += w * o[c].x;
+            acc.y += w * o[c].y;
+            acc.z += w * o[c].z;
+            acc.w += w * o[c].w;
+        }
+    }
+    if (L != L && lane == 0) lorc_set_status(status, LORC_ERR_ARG);
+    if (L == 0.f && lane == 0 && row % ((long long)T * H_q) == 0) lorc_set_status(status, LORC_ERR_EMPTY);
+    const float inv = L > 0.f ? 1.f / L : 0.f;
+    const __nv_bfloat162 x = __floats2bfloat162_rn(acc.x * inv, acc.y * inv), y = __floats2bfloat162_rn(acc.z * inv, acc.w * inv);
+    *reinterpret_cast<uint2*>(out + row * 128 + lane * 4) =
+        make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
 }
 
 }  // namespace
@@ -686,7 +769,10 @@ cudaError_t lorc_tc_prefill_set_attrs() {
     cudaError_t e = cudaFuncSetAttribute(lorc_reconstruct_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                          (int)sizeof(RecSmem) + 1024);
     if (e == cudaSuccess)
-        e = cudaFuncSetAttribute(lorc_prefill_attn_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+        e = cudaFuncSetAttribute(lorc_prefill_attn_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 (int)sizeof(FaSmem) + 1024);
+    if (e == cudaSuccess)
+        e = cudaFuncSetAttribute(lorc_prefill_attn_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                  (int)sizeof(FaSmem) + 1024);
     return e;
 }
@@ -700,7 +786,7 @@ static bool prefill_kv_map(const lorc_ctx* ctx, const void* base, int batch, siz
 }
 
 cudaError_t lorc_tc_prefill_attend(lorc_ctx* ctx, const int32_t* seq_lens, int batch, size_t rows, int max_len, const void* khat, const void* vbuf,
-                                   const bf16* q, bf16* out, int T, cudaStream_t st, int* launches) {
+                                   const bf16* q, bf16* out, int T, int n_split, float* parts, cudaStream_t st, int* launches) {
     const lorc_model_desc& d = ctx->desc;
     CUtensorMap mapQ, mapK, mapV;
     {
@@ -715,9 +801,21 @@ cudaError_t lorc_tc_prefill_attend(lorc_ctx* ctx, const int32_t* seq_lens, int b
     fp.out = out; fp.seq_lens = seq_lens; fp.rope_table = ctx->rope_table; fp.status = ctx->status_dev;
     fp.T = T; fp.H_q = d.n_q_heads; fp.G = ctx->group; fp.n_rows = max_len; fp.max_pos = d.max_pos;
     const int qp = 2 * TILE / ctx->group;                      // query positions per CTA (two blocks of 128 rows)
-    dim3 fgrid((T + qp - 1) / qp, d.n_kv_heads, batch);
+    dim3 fgrid((T + qp - 1) / qp * n_split, d.n_kv_heads, batch);
+    const long long out_rows = (long long)batch * T * d.n_q_heads;
+    fp.n_split = n_split; fp.part_o = parts; fp.part_ml = n_split > 1 ? parts + n_split * out_rows * 128 : nullptr;
     *launches += 1;
-    return lorc_launch_dependent(lorc_prefill_attn_kernel, fgrid, dim3(F_THREADS), sizeof(FaSmem) + 1024, st, mapQ, mapK, mapV, fp);
+    if (n_split == 1)
+        return lorc_launch_dependent(lorc_prefill_attn_kernel<false>, fgrid, dim3(F_THREADS), sizeof(FaSmem) + 1024, st, mapQ, mapK, mapV, fp);
+    cudaError_t e = lorc_launch_dependent(lorc_prefill_attn_kernel<true>, fgrid, dim3(F_THREADS), sizeof(FaSmem) + 1024, st, mapQ, mapK, mapV, fp);
+    if (e != cudaSuccess) return e;
+    *launches += 1;
+    return lorc_launch_dependent(lorc_prefill_merge_kernel, dim3((unsigned)((out_rows + 7) / 8)), dim3(256), 0, st, (const float*)fp.part_ml,
+                                 (const float*)fp.part_o, out, n_split, out_rows, T, d.n_q_heads, ctx->status_dev);
+}
+
+size_t lorc_tc_prefill_part_bytes(const lorc_ctx* ctx, int batch, int T, int n_split) {
+    return n_split > 1 ? (size_t)n_split * batch * T * ctx->desc.n_q_heads * 130 * sizeof(float) : 0;
 }
 
 cudaError_t lorc_tc_prefill_launch(lorc_ctx* ctx, const LorcLayer& L, const CacheView& cv, const CUtensorMap& mapCK,
@@ -750,5 +848,5 @@ cudaError_t lorc_tc_prefill_launch(lorc_ctx* ctx, const LorcLayer& L, const Cach
     *launches += 1;
     if (e != cudaSuccess) return e;
 
-    return lorc_tc_prefill_attend(ctx, cv.seq_lens, cv.batch, rows, (int)rows, khat, vbuf, q, out, T, st, launches);
+    return lorc_tc_prefill_attend(ctx, cv.seq_lens, cv.batch, rows, (int)rows, khat, vbuf, q, out, T, 1, nullptr, st, launches);
 }

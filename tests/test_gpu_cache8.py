@@ -148,6 +148,29 @@ def test_prompt_chunks(kind, heads, fp16, T, lens, page):
     c.close()
 
 
+@pytest.mark.parametrize("kind", H8.KINDS)
+@pytest.mark.parametrize("T,lens,page", [(40, [5000], 0), (70, [70, 2500, 1000], 64), (33, [33, 40, 4000], 16)])
+def test_chunks_behind_long_contexts(kind, T, lens, page):
+    """Few queries and many keys: CTAs share the keys of a block of queries, and some have none of a short sequence's."""
+    import torch
+    c = H8.Case(kind, 32, 8, 128, lens, page=page, seed=T)
+    q, qd = c.queries(T, scale=1.0)
+    out = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device="cuda")
+    c.workspace(T)
+    c.L.lorc_prefill_attn8(c.ctx, 0, c.cache(), qd, out, T)
+    assert c.L.lorc_last_path(c.ctx) == 2
+    H8.assert_attention(H.host_f64(out), *c.want(q, T), fp16=True)
+    assert c.status() == 0 and c.guard_intact()
+    # a sequence that is shorter than the chunk, and one without tokens
+    if len(lens) == 3:
+        c.lens = [T - 1, lens[1], 0]
+        c.sl.copy_(torch.tensor(c.lens, dtype=torch.int32))
+        c.L.lorc_prefill_attn8(c.ctx, 0, c.cache(), qd, out, T)
+        H8.assert_attention(H.host_f64(out), *c.want(q, T), fp16=True)
+        assert not out[0].any() and not out[2].any() and c.status() in (c.L.LORC_ERR_ARG, c.L.LORC_ERR_EMPTY)
+    c.close()
+
+
 @pytest.mark.parametrize("heads", [(32, 8, 128), (4, 2, 64)])
 def test_a_chunk_longer_than_a_sequence(heads):
     import torch
