@@ -72,20 +72,37 @@ size_t expand8_rows(int max_seq_len) { return ((size_t)max_seq_len + 127) / 128 
 
 constexpr int MAX_SPLIT = 16;
 
-// Time of the attention kernel (and its merge) in tenths of a microsecond with the keys of a block of query rows shared by S CTAs: a
-// CTA takes 2.2 us per tile of 128 keys and 4 us before and after, whatever runs beside it; the merge 3 us and its traffic.
-long long attend8_time(const lorc_ctx* ctx, long long blocks, long long tiles, int S) {
-    const long long waves = (blocks * S + ctx->sm_count - 1) / ctx->sm_count;
-    return waves * ((tiles + S - 1) / S * 22 + 40) + (S > 1 ? 30 + blocks * S * 256 * 130 * 8 / 500000 : 0);
-}
+// How the units of the attention kernel run: the first `whole` ones on a CTA each, of the others S CTAs share the keys.
+struct Split8 {
+    long long units, whole;
+    int S;
+    long long time;              // tenths of a microsecond
+};
 
-// CTAs per pair of blocks of query rows: as many as pay.  (One prompt chunk of 256 tokens behind 8000: 152 us with one, 41 with four.)
-int prefill8_split(const lorc_ctx* ctx, int batch, int max_seq_len, int T) {
+// A CTA takes 2.2 us per tile of 128 keys and 4 us before and after, whatever runs beside it; the merge 3 us and its traffic; two
+// launches of the kernel in a row 2 us more than one.  Either all units share their keys among S CTAs, or those that the full rounds of
+// the SMs leave over.  (256 tokens behind 8000: 152 us with one CTA, 70 with two and 46 with eight.  8 x 512 tokens behind 3584, 512
+// units on 148 SMs: 325 us in four rounds, 318 with the last 68 units shared by two CTAs each.)
+Split8 prefill8_split(const lorc_ctx* ctx, int batch, int max_seq_len, int T) {
     const int qp = 256 / ctx->group;
-    const long long blocks = (long long)batch * ctx->desc.n_kv_heads * ((T + qp - 1) / qp), tiles = ((long long)max_seq_len + 127) / 128;
-    int best = 1;
-    for (int S = 2; S <= MAX_SPLIT && 2 * S <= tiles && blocks * S <= 2ll * ctx->sm_count; ++S)
-        if (attend8_time(ctx, blocks, tiles, S) < attend8_time(ctx, blocks, tiles, best)) best = S;
+    const long long P = ctx->sm_count, tiles = ((long long)max_seq_len + 127) / 128;
+    Split8 best;
+    best.units = best.whole = (long long)batch * ctx->desc.n_kv_heads * ((T + qp - 1) / qp);
+    best.S = 1;
+    best.time = (best.units + P - 1) / P * (tiles * 22 + 40);
+    for (int full = 0; full < 2; ++full) {
+        const long long whole = full ? best.units / P * P : 0, rest = best.units - whole;
+        if (rest == 0 || (full && whole == 0)) continue;
+        for (int S = 2; S <= MAX_SPLIT && 2 * S <= tiles && rest * S <= 2 * P; ++S) {
+            const long long time = whole / P * (tiles * 22 + 40) + (rest * S + P - 1) / P * ((tiles + S - 1) / S * 22 + 40) + 30 +
+                                   rest * S * LORC_PREFILL_PART_FLOATS * 8 / 500000 + (full ? 20 : 0);
+            if (time < best.time) {
+                best.whole = whole;
+                best.S = S;
+                best.time = time;
+            }
+        }
+    }
     return best;
 }
 
@@ -100,23 +117,22 @@ size_t expand8_bytes(const lorc_ctx* ctx, int batch, int max_seq_len) {
 // tokens, 8B shape, 4 queries 43 us against 112, 16 queries 147 against 108; one sequence of 1000 tokens, 32 queries 16 against 26).
 bool lorc_prefill8_supported(const lorc_ctx* ctx, const Cache8View& cv, int T) {
     if (T == 1 || cv.batch > 65535 || !lorc_tc_prefill_shape_ok(ctx) || (ctx->desc.flags & LORC_FLAG_DEBUG_FP32)) return false;
-    const int qp = 256 / ctx->group;
-    const long long blocks = (long long)cv.batch * cv.n_kv * ((T + qp - 1) / qp), tiles = ((long long)cv.max_seq_len + 127) / 128;
     const long long units = (long long)cv.batch * cv.n_kv * ((cv.max_seq_len + 63) / 64), P = ctx->sm_count;
     const long long stream = 80 + 33 * units * T / (10 * P);
-    const long long expand = 100 + 13 * units / P + attend8_time(ctx, blocks, tiles, prefill8_split(ctx, cv.batch, cv.max_seq_len, T));
+    const long long expand = 100 + 13 * units / P + prefill8_split(ctx, cv.batch, cv.max_seq_len, T).time;
     return expand < stream;
 }
 
 size_t lorc_prefill8_scratch_bytes(const lorc_ctx* ctx, int batch, int max_seq_len, int T) {
-    return expand8_bytes(ctx, batch, max_seq_len) +
-           lorc_tc_prefill_part_bytes(ctx, batch, T, prefill8_split(ctx, batch, max_seq_len, T));
+    const Split8 split = prefill8_split(ctx, batch, max_seq_len, T);
+    return expand8_bytes(ctx, batch, max_seq_len) + (size_t)(split.units - split.whole) * split.S * LORC_PREFILL_PART_FLOATS * sizeof(float);
 }
 
 size_t lorc_prefill8_scratch_most(const lorc_ctx* ctx, int batch, int max_seq_len, int T) {
-    // a call with fewer tokens may share their keys among more CTAs: at most MAX_SPLIT, and two blocks of 256 rows per SM
-    const size_t rows = (size_t)batch * T * ctx->desc.n_q_heads * MAX_SPLIT, cap = 2 * (size_t)ctx->sm_count * 256;
-    return expand8_bytes(ctx, batch, max_seq_len) + (rows < cap ? rows : cap) * 130 * sizeof(float);
+    // a call with fewer sequences or tokens may share more units' keys, among more CTAs: two per SM at most, and MAX_SPLIT per unit
+    const size_t qp = 256 / ctx->group, all = (size_t)batch * ctx->desc.n_kv_heads * ((T + qp - 1) / qp) * MAX_SPLIT;
+    const size_t cap = 2 * (size_t)ctx->sm_count;
+    return expand8_bytes(ctx, batch, max_seq_len) + (all < cap ? all : cap) * LORC_PREFILL_PART_FLOATS * sizeof(float);
 }
 
 cudaError_t lorc_prefill8_launch(lorc_ctx* ctx, const Cache8View& cv, const bf16* q, bf16* out, int T, void* scratch,
@@ -141,6 +157,7 @@ cudaError_t lorc_prefill8_launch(lorc_ctx* ctx, const Cache8View& cv, const bf16
                                     : lorc_launch_dependent(expand8_kernel<false>, grid, dim3(256), 0, st, p);
     *launches += 1;
     if (e != cudaSuccess) return e;
-    return lorc_tc_prefill_attend(ctx, cv.seq_lens, cv.batch, rows, cv.max_seq_len, p.khat, p.vbuf, q, out, T,
-                                  prefill8_split(ctx, cv.batch, cv.max_seq_len, T), (float*)((char*)scratch + kv), st, launches);
+    const Split8 split = prefill8_split(ctx, cv.batch, cv.max_seq_len, T);
+    return lorc_tc_prefill_attend(ctx, cv.seq_lens, cv.batch, rows, cv.max_seq_len, p.khat, p.vbuf, q, out, T, split.whole, split.S,
+                                  (float*)((char*)scratch + kv), st, launches);
 }

@@ -98,12 +98,13 @@ cudaError_t lorc_tc_prefill_launch(lorc_ctx* ctx, const LorcLayer& L, const Cach
                                    const CUtensorMap& mapCV, const CUtensorMap* mapBKT, const CUtensorMap* mapBVT,
                                    const bf16* q, bf16* out, int T, void* scratch, cudaStream_t st, int* launches);
 // Its second half: the attention over keys (rotated) and values [batch, rows, n] in fp16, rows a multiple of 128.  A
-// sequence of more than max_len tokens is treated as empty (and reported).  n_split > 1: that many CTAs share the keys of a query
-// block, with lorc_tc_prefill_part_bytes of scratch for what they leave to a merge kernel.
-size_t lorc_tc_prefill_part_bytes(const lorc_ctx* ctx, int batch, int T, int n_split);
+// sequence of more than max_len tokens is treated as empty (and reported).  A unit is two blocks of 128 query
+// rows of a KV head; n_split > 1: of the units behind the first `whole` ones that many CTAs share the keys, with
+// LORC_PREFILL_PART_FLOATS of scratch per unit and CTA for what they leave to a merge kernel.
+#define LORC_PREFILL_PART_FLOATS (256 * 130)
 cudaError_t lorc_tc_prefill_attend(lorc_ctx* ctx, const int32_t* seq_lens, int batch, size_t rows, int max_len, const void* khat,
-                                   const void* vbuf, const bf16* q, bf16* out, int T, int n_split, float* parts, cudaStream_t st,
-                                   int* launches);
+                                   const void* vbuf, const bf16* q, bf16* out, int T, long long whole, int n_split, float* parts,
+                                   cudaStream_t st, int* launches);
 cudaError_t lorc_tc_prefill(lorc_ctx* ctx, int layer, const LorcLayer& L, const CacheView& cv, const bf16* q, bf16* out,
                             int T, void* ws, size_t ws_bytes, cudaStream_t st, int* launches);
 

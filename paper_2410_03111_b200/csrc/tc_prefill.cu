@@ -337,9 +337,10 @@ struct FaParams {
     const float2* rope_table;      // [max_pos][64]
     int* status;
     int T, H_q, G, n_rows, max_pos;
-    int n_split;                   // SPLIT: CTAs that share the keys of two blocks of query rows
-    float* part_ml;                // SPLIT: [n_split][b, T, H_q][2] reference, sum of the row's probabilities
-    float* part_o;                 // SPLIT: [n_split][b, T, H_q][128] un-normalised output
+    int nx, n_kv, unit0;           // CTAs of a sequence and KV head (a unit each, numbered in the order x, KV head, sequence); the launch's first
+    int n_split;                   // SPLIT: CTAs that share the keys of a unit
+    float* part_ml;                // SPLIT: [unit][n_split][256 rows][2] reference, sum of the row's probabilities
+    float* part_o;                 // SPLIT: [unit][n_split][256 rows][128] un-normalised output
 };
 
 __device__ __forceinline__ float ex2_approx(float x) {
@@ -364,7 +365,7 @@ __device__ __forceinline__ void probs_chunk(const uint32_t (&r)[32], float m, ui
     tmem_st16(taddr, w);
 }
 
-// SPLIT: n_split CTAs share the key tiles of the two blocks of query rows (where there are fewer blocks than SMs), in contiguous
+// SPLIT: n_split CTAs share the key tiles of the two blocks of query rows (where there are too few blocks for the SMs), in contiguous
 // equal parts; each leaves its rows' references, sums and un-normalised outputs for a merge kernel.
 template <bool SPLIT>
 __global__ void __launch_bounds__(F_THREADS, 1)
@@ -373,12 +374,12 @@ lorc_prefill_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_
     extern __shared__ uint8_t raw[];
     FaSmem& sm = *reinterpret_cast<FaSmem*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
-    const int g = blockIdx.y, s = blockIdx.z;
+    const int local = SPLIT ? (int)blockIdx.x / p.n_split : (int)blockIdx.x, unit = p.unit0 + local;
+    const int part = SPLIT ? (int)blockIdx.x - local * p.n_split : 0;
+    const int g = unit / p.nx % p.n_kv, s = unit / (p.nx * p.n_kv);
     const int qp = TILE / p.G;                                // query positions per block of 128 rows
     // the CTAs with the latest positions see the most keys: they go first
-    const int bx = SPLIT ? (int)blockIdx.x / p.n_split : (int)blockIdx.x, nx = SPLIT ? (int)gridDim.x / p.n_split : (int)gridDim.x;
-    const int part = SPLIT ? (int)blockIdx.x - bx * p.n_split : 0;
-    const int t0 = (nx - 1 - bx) * 2 * qp;                    // first position (inside the chunk) of this CTA
+    const int t0 = (p.nx - 1 - unit % p.nx) * 2 * qp;         // first position (inside the chunk) of this CTA
     if (tid == 0) {
         mbar_init(&sm.q_full, 1);
         mbar_init(&sm.q_ready, 8);
@@ -647,7 +648,7 @@ lorc_prefill_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_
             const bool has_out = t0 + tt < p.T;                // (rows past the chunk still take part in the warp-wide loads)
             const float l = l0 + l1;
             if (SPLIT) {
-                const long long at = (((long long)part * gridDim.z + s) * p.T + (has_out ? t0 + tt : 0)) * p.H_q + g * p.G + hi;
+                const long long at = (((long long)local * p.n_split + part) * 2 + b) * TILE + row;
                 if (has_out) *reinterpret_cast<float2*>(p.part_ml + at * 2) = make_float2(m_ref, l);
                 if (n_tiles > 0) {
 #pragma unroll 1
@@ -698,15 +699,19 @@ lorc_prefill_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_
     if (warp == 1) tmem_dealloc(tmem, 512);
 }
 
-// Merge of the parts of a row (b, t, head): one warp per row, four dimensions per lane.
+// Merge of the parts of a row: one warp per row, four dimensions per lane.
 __global__ void __launch_bounds__(256)
-lorc_prefill_merge_kernel(const float* __restrict__ part_ml, const float* __restrict__ part_o, bf16* __restrict__ out, int n_split,
-                          long long rows, int T, int H_q, int* status) {
-    const int lane = threadIdx.x & 31;
-    const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+lorc_prefill_merge_kernel(const FaParams p) {
+    const int lane = threadIdx.x & 31, r = (int)blockIdx.x % 32 * 8 + (threadIdx.x >> 5), local = (int)blockIdx.x / 32;
+    const int unit = p.unit0 + local, g = unit / p.nx % p.n_kv, s = unit / (p.nx * p.n_kv), qp = TILE / p.G;
+    const int t = (p.nx - 1 - unit % p.nx) * 2 * qp + (r >= TILE ? qp : 0) + r % TILE / p.G, n_split = p.n_split;
     grid_dep_wait();
     grid_dep_launch();
-    if (row >= rows) return;
+    if (t >= p.T) return;
+    const float* part_ml = p.part_ml + (long long)local * n_split * 2 * TILE * 2;
+    const float* part_o = p.part_o + (long long)local * n_split * 2 * TILE * 128;
+    constexpr long long rows = 2 * TILE;
+    const int row = r;
     float M = -INFINITY, L = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int c0 = 0; c0 < n_split; c0 += 4) {
@@ -743,11 +748,11 @@ lorc_prefill_merge_kernel(const float* __restrict__ part_ml, const float* __rest
             acc.w += w * o[c].w;
         }
     }
-    if (L != L && lane == 0) lorc_set_status(status, LORC_ERR_ARG);
-    if (L == 0.f && lane == 0 && row % ((long long)T * H_q) == 0) lorc_set_status(status, LORC_ERR_EMPTY);
+    if (L != L && lane == 0) lorc_set_status(p.status, LORC_ERR_ARG);
+    if (L == 0.f && lane == 0 && t == 0) lorc_set_status(p.status, LORC_ERR_EMPTY);
     const float inv = L > 0.f ? 1.f / L : 0.f;
     const __nv_bfloat162 x = __floats2bfloat162_rn(acc.x * inv, acc.y * inv), y = __floats2bfloat162_rn(acc.z * inv, acc.w * inv);
-    *reinterpret_cast<uint2*>(out + row * 128 + lane * 4) =
+    *reinterpret_cast<uint2*>(p.out + (((long long)s * p.T + t) * p.H_q + g * p.G + r % p.G) * 128 + lane * 4) =
         make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
 }
 
@@ -786,7 +791,8 @@ static bool prefill_kv_map(const lorc_ctx* ctx, const void* base, int batch, siz
 }
 
 cudaError_t lorc_tc_prefill_attend(lorc_ctx* ctx, const int32_t* seq_lens, int batch, size_t rows, int max_len, const void* khat, const void* vbuf,
-                                   const bf16* q, bf16* out, int T, int n_split, float* parts, cudaStream_t st, int* launches) {
+                                   const bf16* q, bf16* out, int T, long long whole, int n_split, float* parts, cudaStream_t st,
+                                   int* launches) {
     const lorc_model_desc& d = ctx->desc;
     CUtensorMap mapQ, mapK, mapV;
     {
@@ -801,21 +807,23 @@ cudaError_t lorc_tc_prefill_attend(lorc_ctx* ctx, const int32_t* seq_lens, int b
     fp.out = out; fp.seq_lens = seq_lens; fp.rope_table = ctx->rope_table; fp.status = ctx->status_dev;
     fp.T = T; fp.H_q = d.n_q_heads; fp.G = ctx->group; fp.n_rows = max_len; fp.max_pos = d.max_pos;
     const int qp = 2 * TILE / ctx->group;                      // query positions per CTA (two blocks of 128 rows)
-    dim3 fgrid((T + qp - 1) / qp * n_split, d.n_kv_heads, batch);
-    const long long out_rows = (long long)batch * T * d.n_q_heads;
-    fp.n_split = n_split; fp.part_o = parts; fp.part_ml = n_split > 1 ? parts + n_split * out_rows * 128 : nullptr;
-    *launches += 1;
-    if (n_split == 1)
-        return lorc_launch_dependent(lorc_prefill_attn_kernel<false>, fgrid, dim3(F_THREADS), sizeof(FaSmem) + 1024, st, mapQ, mapK, mapV, fp);
-    cudaError_t e = lorc_launch_dependent(lorc_prefill_attn_kernel<true>, fgrid, dim3(F_THREADS), sizeof(FaSmem) + 1024, st, mapQ, mapK, mapV, fp);
+    fp.nx = (T + qp - 1) / qp; fp.n_kv = d.n_kv_heads; fp.unit0 = 0; fp.n_split = 1;
+    const long long units = (long long)fp.nx * d.n_kv_heads * batch;
+    if (n_split == 1) whole = units;
+    if (units * n_split > 0x7fffffffll / 32) return cudaErrorInvalidValue;
+    if (whole > 0) {
+        *launches += 1;
+        cudaError_t e = lorc_launch_dependent(lorc_prefill_attn_kernel<false>, dim3((unsigned)whole), dim3(F_THREADS), sizeof(FaSmem) + 1024, st,
+                                              mapQ, mapK, mapV, fp);
+        if (e != cudaSuccess || whole == units) return e;
+    }
+    const long long rest = units - whole;
+    fp.unit0 = (int)whole; fp.n_split = n_split; fp.part_o = parts; fp.part_ml = parts + rest * n_split * 2 * TILE * 128;
+    *launches += 2;
+    cudaError_t e = lorc_launch_dependent(lorc_prefill_attn_kernel<true>, dim3((unsigned)(rest * n_split)), dim3(F_THREADS), sizeof(FaSmem) + 1024,
+                                          st, mapQ, mapK, mapV, fp);
     if (e != cudaSuccess) return e;
-    *launches += 1;
-    return lorc_launch_dependent(lorc_prefill_merge_kernel, dim3((unsigned)((out_rows + 7) / 8)), dim3(256), 0, st, (const float*)fp.part_ml,
-                                 (const float*)fp.part_o, out, n_split, out_rows, T, d.n_q_heads, ctx->status_dev);
-}
-
-size_t lorc_tc_prefill_part_bytes(const lorc_ctx* ctx, int batch, int T, int n_split) {
-    return n_split > 1 ? (size_t)n_split * batch * T * ctx->desc.n_q_heads * 130 * sizeof(float) : 0;
+    return lorc_launch_dependent(lorc_prefill_merge_kernel, dim3((unsigned)(rest * 32)), dim3(256), 0, st, fp);
 }
 
 cudaError_t lorc_tc_prefill_launch(lorc_ctx* ctx, const LorcLayer& L, const CacheView& cv, const CUtensorMap& mapCK,
@@ -848,5 +856,5 @@ cudaError_t lorc_tc_prefill_launch(lorc_ctx* ctx, const LorcLayer& L, const Cach
     *launches += 1;
     if (e != cudaSuccess) return e;
 
-    return lorc_tc_prefill_attend(ctx, cv.seq_lens, cv.batch, rows, (int)rows, khat, vbuf, q, out, T, 1, nullptr, st, launches);
+    return lorc_tc_prefill_attend(ctx, cv.seq_lens, cv.batch, rows, (int)rows, khat, vbuf, q, out, T, 0, 1, nullptr, st, launches);
 }
