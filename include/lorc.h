@@ -291,6 +291,8 @@ int lorc_decode_step_host(lorc_ctx* ctx, int layer, const lorc_cache* cache, con
  * blocks wholly behind it, are neither read into a result nor written.
  * A sequence longer than max_seq_len, the capacity or max_pos counts as empty (status CAPACITY); tokens whose page lies
  * outside the pool are left out (CAPACITY too).
+ * With LORC_FLAG_DEBUG_FP32 the projection runs on the plain kernel and attention keeps off the tcgen05 kernels (it has no
+ * plain form: its products are exact and its sums fp32 in any case).
  * The calls need a loaded FULL layer and the context's device to be the current one, and like lorc_decode_attn those of one
  * context must not overlap on the GPU: they share its workspace. */
 #define LORC_CACHE8_INT8 0      /* signed integers from -127 to 127 */
@@ -410,8 +412,8 @@ int lorc_sync_status(lorc_ctx* ctx, void* stream);
 /* Text of the last error reported on this context (never NULL). */
 const char* lorc_last_error(const lorc_ctx* ctx);
 
-/* Which kernel family the last lorc_decode_attn / lorc_append call on this
- * context used: 0 = none yet, 1 = plain kernels (fp32 arithmetic; outside the debug flag
+/* Which kernel family the last lorc_decode_attn / lorc_append call (or their prompt and
+ * 8-bit forms) on this context used: 0 = none yet, 1 = plain kernels (fp32 arithmetic; outside the debug flag
  * the key reconstruction of decode steps runs on mma.sync), 2 = tensor-core
  * (tcgen05) kernels of the latent mode, 3 = warp-level tensor-core (mma.sync) kernel of
  * the uncompressed mode.  For tests and benchmarks. */

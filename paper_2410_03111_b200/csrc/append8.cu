@@ -220,7 +220,7 @@ cudaError_t lorc_append8_launch(lorc_ctx* ctx, const LorcLayer& L, const Cache8V
     p.n_blocks = (T + LORC_BLOCK8 - 2) / LORC_BLOCK8 + 1;
     p.interleaved = ctx->pair_style == LORC_ROPE_INTERLEAVED;
     if (lorc_append8_tc_supported(ctx, cv.batch, T)) return lorc_append8_tc_launch(ctx, L, p, x, st, launches);
-    const bool mma = D % 256 == 0 && L.A_tiled != nullptr;
+    const bool mma = D % 256 == 0 && L.A_tiled != nullptr && !(ctx->desc.flags & LORC_FLAG_DEBUG_FP32);
     // grid rows are limited to 65535: chunks of as many tokens
     const int tile = mma ? 16 : 8;
     const long long most = 65535ll * tile;

@@ -57,6 +57,97 @@ def test_decode_long_and_ragged(kind):
         c.close()
 
 
+def test_decode_of_many_sequences():
+    """More sequences than one look at the lengths covers, with parts that begin and end inside them, and empty ones among them."""
+    rng = np.random.default_rng(6)
+    lens = [int(x) for x in rng.integers(1, 600, 170)]
+    for heads in ((4, 1, 64), (8, 8, 64)):
+        c = H8.Case("int8", *heads, lens, page=16, D=64, seed=60, max_len=600)
+        q, got = _decode(c)
+        want = c.want(q)
+        H8.assert_attention(got, *want)
+        assert c.status() == 0 and c.guard_intact()
+        import torch
+        for s in (0, 31, 32, 128, 150, 169):
+            c.lens[s] = 0
+            for w in want:
+                w[s] = 0.0
+        c.sl.copy_(torch.tensor(c.lens, dtype=torch.int32))
+        out = torch.full((c.b, c.H_q, c.d_h), 7.0, dtype=torch.bfloat16, device="cuda")
+        c.L.lorc_decode_attn8(c.ctx, 0, c.cache(), H.dev_bf16(q[:, 0]), out)
+        H8.assert_attention(H.host_f64(out).reshape(got.shape), *want)
+        assert c.status() == c.L.LORC_ERR_EMPTY
+        c.close()
+
+
+def test_a_pool_beyond_32_bit_offsets():
+    """Pages more than 2^32 bytes into a pool: write, both attentions, fork and compaction reach them."""
+    import torch
+    L = H.lib()
+    n_pages, ps, n = 36000, 128, 1024
+    kv = torch.zeros(2, n_pages, ps, n, dtype=torch.int8, device="cuda")
+    sc = torch.zeros(2, n_pages, ps // 16, 8, device="cuda")
+    small = H8.Case("int8", 32, 8, 128, [300, 140], page=ps, D=256, seed=61)
+    far = torch.tensor([[n_pages - 1, n_pages - 7, n_pages - 3], [n_pages - 2, n_pages - 9, n_pages - 4]], dtype=torch.int32, device="cuda")
+    kv[:, far.flatten().long()] = small.kv[:, small.table.flatten().long()]
+    sc[:, far.flatten().long()] = small.sc[:, small.table.flatten().long()]
+    cache = L.make_cache8(kv[0], kv[1], sc[0], sc[1], small.sl, 2, 300, L.LORC_CACHE8_INT8, page_table=far, page_size=ps,
+                          max_pages_per_seq=3, n_pages=n_pages)
+    small.workspace(100)
+    x = H.dev_bf16(small.rng.standard_normal((2, 100, 256)))
+    q = H.dev_bf16(small.rng.standard_normal((2, 100, 32, 128)))
+    outs = []
+    for c in (small.cache(), cache):
+        out, dec = torch.zeros_like(q), torch.zeros(2, 32, 128, dtype=torch.bfloat16, device="cuda")
+        L.lorc_append8(small.ctx, 0, c, x, 100)
+        L.lorc_append8(small.ctx, 0, c, x[:, 99:].contiguous(), 1)
+        L.lorc_prefill_attn8(small.ctx, 0, c, q, out, 100)
+        L.lorc_decode_attn8(small.ctx, 0, c, q[:, 0].contiguous(), dec)
+        outs.append((out, dec))
+    assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
+    assert torch.equal(kv[:, far.flatten().long()], small.kv[:, small.table.flatten().long()])
+    assert small.status() == 0
+    refs = torch.zeros(n_pages, dtype=torch.int32, device="cuda")
+    refs[far.flatten().long()] = 1
+    table = torch.cat([far, torch.full_like(far, -1)])
+    lens = torch.tensor([300, 384, 0, 0], dtype=torch.int32, device="cuda")
+    pages = L.make_pages([kv[0], kv[1], sc[0], sc[1]], table, lens, refs, ps)
+    ws = torch.zeros(L.lorc_pages_workspace_bytes(pages, 2), dtype=torch.uint8, device="cuda")
+    L.lorc_set_workspace(small.ctx, ws)
+    want = [kv[:, far[0].long()].clone(), sc[:, far[1].long()].clone()]
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    L.lorc_pages_fork(small.ctx, pages, i32([0]), i32([2]), 1)
+    assert int(table[2, 2]) == 0 and torch.equal(kv[:, 0], kv[:, n_pages - 3])
+    L.lorc_pages_compact(small.ctx, pages)
+    assert torch.equal(kv[:, table[0].long()], want[0]) and torch.equal(sc[:, table[1].long()], want[1])
+    assert int(table.max()) == 6 and small.status() == 0
+    small.close()
+
+
+@pytest.mark.parametrize("kind", H8.KINDS)
+def test_the_debug_flag_keeps_the_results(kind):
+    """The plain projection and the attention off the tcgen05 kernels: within the same bounds."""
+    import torch
+    c = H8.Case(kind, 32, 8, 128, [130, 517], page=64, seed=62, flags=H.lib().LORC_FLAG_DEBUG_FP32, style=H.ROPE_NONE)
+    at, x = _exact_x(c, 130)
+    c.workspace(130)
+    c.L.lorc_append8(c.ctx, 0, c.cache(), x, 130)
+    assert c.L.lorc_last_path(c.ctx) == 1
+    c.codes, c.scales = H8.host_codes(c.kv, kind), c.sc.double().cpu().numpy()
+    for s, n in enumerate(c.lens):
+        new = np.asarray(c.w[1], dtype=np.float64)[at[s]].reshape(130, c.H_kv, c.d_h)
+        page, row = c.rows_of(s, n)
+        step = c.scales[1][page, row // 16][n - 130:][..., None]
+        assert (np.abs(c.held(1, s, n)[n - 130:] - new) <= (step / 2 if kind == "int8" else np.maximum(2.0 ** -4 * np.abs(new), step * 2.0 ** -10))).all()
+    q, qd = c.queries(130, scale=1.0)
+    out = torch.zeros(q.shape, dtype=torch.bfloat16, device="cuda")
+    c.L.lorc_prefill_attn8(c.ctx, 0, c.cache(), qd, out, 130)
+    assert c.L.lorc_last_path(c.ctx) == 3
+    H8.assert_attention(H.host_f64(out), *c.want(q, 130))
+    assert c.status() == 0
+    c.close()
+
+
 @pytest.mark.parametrize("kind", H8.KINDS)
 def test_decode_scales_of_any_size(kind):
     """Scales that are no powers of two, differ by 2^40 between blocks, or are zero."""
