@@ -235,7 +235,11 @@ append8_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constan
                 if (++st == A8_STAGES) { st = 0; par ^= 1; }
             }
         }
-        if (!ok && lane == 0) lorc_set_status(p.q.status, LORC_ERR_TIMEOUT);
+        if (!ok) {
+            // copies may be under way into either CTA: neither leaves before they must have landed
+            if (lane == 0) lorc_set_status(p.q.status, LORC_ERR_TIMEOUT);
+            for (const uint64_t since = global_timer_ns(); global_timer_ns() - since < 1000000ull;) {}
+        }
     } else if (warp == 1) {
         // ------------------------------------------------------------------ MMA issuer (leader CTA only)
         // A: x rows (K-major), a k-step is 32 bytes.  B: factor blocks (MN-major: a D row's 64 columns are contiguous),
