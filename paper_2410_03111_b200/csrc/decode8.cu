@@ -662,7 +662,8 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
                     *reinterpret_cast<float4*>(p.part_o + unit * DH + d) = acc;
                 }
             }
-            if (h0 + 4 < G) asm volatile("bar.sync 1, 128;" ::: "memory");
+            // all have read before a warp writes here again: the other heads, or a short row that comes next
+            asm volatile("bar.sync 1, 128;" ::: "memory");
         }
         if (!whole) {
             // The row's parts c0 .. c1 count themselves in (the counter of c0, since a part begins at most one row that it does not
