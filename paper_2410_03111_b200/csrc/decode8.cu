@@ -1,23 +1,33 @@
 // Attention over the 8-bit cache of uncompressed layers, one query per sequence and head, on the warp-level tensor cores.
 //
-// One pass over 2 n bytes per token, bound by HBM: a block streams (sequence, KV head) pairs; a producer warp keeps
-// D8_STAGES 64-token stages of codes in flight by TMA, each of four consumer warps owns 16 of a stage's tokens, which is one block of
-// the cache: one scale for its keys, one for its values.  Scores and outputs are computed transposed (tokens, then dimensions on
-// the M side of the m16n8k16 tiles, the G <= 8 query heads on the N side).  Codes become fp16 numbers exactly, in registers:
+// One pass over 2 n bytes per token, bound by HBM: a block streams (sequence, KV head) pairs; a producer warp keeps D8_STAGES
+// 128-token stages of codes in flight by TMA, and each of four consumer warps takes 32 of a stage's tokens, two blocks of the cache
+// with a scale each for their keys and values.  A warp of its own rotates the queries of the next sequence.  Scores and outputs are
+// computed transposed (tokens, then dimensions on the M side of the m16n8k16 tiles, the G <= 8 query heads on the N side: tiles of
+// the tcgen05 kind would be 128 wide there).  Codes become fp16 numbers exactly, in registers:
 //
 //   S^T[16 tok x 8] = K[16 tok x d] . Q^^T      Q^ = RoPE(q, N-1) brought to [1, 2) by a power of two per head, in two fp16 parts
 //                                               (22 bits); the scale of the keys, 1 / sqrt(d) and log2 e multiply the fp32 sums
-//   p = 2^(S - m), l += p                       m is raised when a score exceeds it by more than 2^8
-//   O^T[d x 8]     += V^T[d x 16 tok] . (c p)^T c = scale of the values / largest one so far, c p in two fp16 parts
+//   l += 2^(S - m)
+//   O^T[d x 8]     += V^T[d x 16 tok] . Y^T     Y = c 2^(S - w) in one fp16 part, c the scale of the values: each weight is
+//                                               off by 2^-11 at most, which averages out over tokens; bf16 outputs lose 2^-8
+//
+// m and w are raised when they are exceeded by more than 2^8.
 //
 // A 16-bit word of a row is two dimensions.  Key fragments take the dimensions in the order in which ldmatrix delivers bytes, and the
 // query fragments take the same order; for the values a transposed 8 x 8 matrix of words holds two dimensions of two tokens per
 // register, whose bytes are paired by token: fragment row g is dimension 2 g of the 16, row g + 8 dimension 2 g + 1.
 //
-// The steps (64 tokens) of all sequences form one list, cut into equal parts for the blocks of a KV head that are resident at
+// Units of 64 tokens of all sequences form one list, cut into equal parts for the blocks of a KV head that are resident at
 // once: all of them stream from the start to the end of the launch whatever the lengths are.  A part may begin and end inside
 // a sequence; what it computes of a sequence that it does not hold alone goes to memory, un-normalised, and the last of the
-// sequence's parts to get there adds them up.  (A merge kernel of its own cost 6 to 8 us more.)
+// sequence's parts to get there adds them up.  (A merge kernel of its own cost 6 to 8 us more; the same by the queries' warp, so that
+// the others go on, 1 to 3 us more, since one warp takes longer over it at the end of the launch.)
+//
+// Measured, 8 KV heads of 128 dimensions: 16 x 4129 tokens 30 us (4.5 TB/s), 4 x 32777 49 us (5.5), 64 sequences of 512 to
+// 16384 185 us (6.0; a copy 6.6), 128 x 300 31 us: there it is the 1.5 us per sequence and block from its last tile's
+// arrival to the next one's first products.  (Query fragments made by the queries' warp save 1 us of the 31 and cost 1.5 of the
+// 44 of 256 x 200.)
 #include <math.h>
 
 #include "cache8.cuh"
@@ -33,7 +43,7 @@ constexpr int D8_UNIT = 64;          // tokens by which work is dealt out
 constexpr int D8_STAGES = 3;
 constexpr int D8_THREADS = 192;      // warps 0..3 consumers, warp 4 TMA and scales, warp 5 queries
 constexpr int D8_BLOCKS_PER_SM = 2;
-constexpr float D8_RAISE = 8.f;
+constexpr float D8_RAISE = 8.f, D8_SPAN = 120.f;
 constexpr float LOG2E = 1.4426950408889634f;
 
 __device__ __forceinline__ void ldmatrix_x4(uint32_t (&r)[4], uint32_t addr) {
@@ -73,12 +83,15 @@ __device__ __forceinline__ float ex2_approx(float x) {
     return y;
 }
 
+// log2 |x| of a scale, -infinity for zero (absolute error below 2^-15, a thirtieth of what a weight loses as an fp16 number)
+__device__ __forceinline__ float d8_log2(float x) { return __log2f(fabsf(x)); }
+
 template <int DH>
 struct D8Smem {
     uint8_t kv[D8_STAGES][2][D8_TILE * DH];     // keys, values of a stage: rows of DH bytes, swizzled (128 or 64 bytes)
     float o[4][4][DH + 4];                      // at the end of a sequence's part: every warp's un-normalised output, four heads at a time
     float qs[8][DH];                            // rotated queries of the G heads (rows G..7 zero)
-    float m[4][8], l[4][8], vs[4];
+    float m[4][8], l[4][8], w[4][8];
     int last;
     alignas(16) float scale[D8_STAGES][2][D8_TILE / 16];    // scales of a stage's blocks, keys and values
     uint64_t full[D8_STAGES], empty[D8_STAGES], q_full, q_empty;
@@ -499,7 +512,7 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) o[ks][0] = o[ks][1] = o[ks][2] = o[ks][3] = 0.f;
         float m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};   // heads 2 t, 2 t + 1 (l: this lane's tokens)
-        float v_ref = 0.f, v_inv = 0.f;          // largest scale of values so far: o is in units of it
+        float w_run[2] = {-INFINITY, -INFINITY}, m_to_w[2] = {0.f, 0.f};  // o is in units of 2^w; 2^(m - w)
 
         for (int t0 = t_begin; t0 < t_end && ok; t0 += D8_TILE) {
             const int tw = t0 + warp * 32;       // first token of this warp
@@ -552,31 +565,38 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
                     __syncwarp();
                 }
             }
-            // running softmax over this warp's tokens: the reference is raised when a score exceeds it by more than 2^8, which
-            // after the first steps is rare, so the maximum is looked for only then
-            const float top0 = fmaxf(fmaxf(x[0][0], x[0][2]), fmaxf(x[1][0], x[1][2]));
-            const float top1 = fmaxf(fmaxf(x[0][1], x[0][3]), fmaxf(x[1][1], x[1][3]));
-            const float v_mag = fmaxf(fabsf(v_scale[0]), fabsf(v_scale[1]));
-            if (__any_sync(0xffffffffu, top0 > m_run[0] + D8_RAISE || top1 > m_run[1] + D8_RAISE || v_mag > v_ref)) {
-                float shrink = 1.f;
-                if (v_mag > v_ref) {
-                    const float now = fmaxf(v_mag, 1e-35f);
-                    v_inv = 1.f / now;
-                    shrink = v_ref * v_inv;
-                    v_ref = now;
-                }
+            // Running softmax over this warp's tokens.  The sum of p and the weighted values have references of their own (m, w): a
+            // token's weight is p times its values' scale, so tokens with small values count in full also beside tokens of little
+            // weight with far larger values.  A reference is raised when it is exceeded by more than 2^8, which after the
+            // first steps is rare, so the maximum over the warp is looked for only then.
+            const float lv[2] = {d8_log2(v_scale[0]), d8_log2(v_scale[1])};
+            float top[2], heavy[2];              // the largest score, and the largest weight (score + log2 of the scale), heads 2 t, 2 t + 1
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float a = fmaxf(x[0][e], x[0][2 + e]), b = fmaxf(x[1][e], x[1][2 + e]);
+                top[e] = fmaxf(a, b);
+                heavy[e] = fmaxf(a + lv[0], b + lv[1]);
+            }
+            if (__any_sync(0xffffffffu, top[0] > m_run[0] + D8_RAISE || top[1] > m_run[1] + D8_RAISE || heavy[0] > w_run[0] + D8_RAISE ||
+                                            heavy[1] > w_run[1] + D8_RAISE)) {
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float mx = e ? top1 : top0;
 #pragma unroll
-                    for (int d = 4; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-                    float alpha = 1.f;
-                    if (mx > m_run[e] + D8_RAISE) {
-                        alpha = m_run[e] == -INFINITY ? 0.f : ex2_approx(m_run[e] - mx);
-                        m_run[e] = mx;
+                    for (int d = 4; d < 32; d <<= 1) {
+                        top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], d));
+                        heavy[e] = fmaxf(heavy[e], __shfl_xor_sync(0xffffffffu, heavy[e], d));
                     }
-                    l_run[e] *= alpha;
-                    alpha *= shrink;
+                    if (top[e] > m_run[e] + D8_RAISE) {
+                        l_run[e] *= m_run[e] == -INFINITY ? 0.f : ex2_approx(m_run[e] - top[e]);
+                        m_run[e] = top[e];
+                    }
+                    // (2^(m - w) stays a number of fp32: w is at least m - D8_SPAN, and at most m + D8_SPAN, which only scales beyond
+                    // 2^(D8_SPAN - D8_RAISE) could exceed)
+                    float now = heavy[e] > w_run[e] + D8_RAISE ? heavy[e] : w_run[e];
+                    if (m_run[e] != -INFINITY) now = fminf(fmaxf(now, m_run[e] - D8_SPAN), m_run[e] + D8_SPAN);
+                    const float alpha = w_run[e] == -INFINITY ? 0.f : ex2_approx(w_run[e] - now);
+                    w_run[e] = now;
+                    m_to_w[e] = m_run[e] == -INFINITY ? 0.f : ex2_approx(m_run[e] - now);
 #pragma unroll
                     for (int ks = 0; ks < KS; ++ks) {
                         o[ks][e] *= alpha;
@@ -584,18 +604,18 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
                     }
                 }
             }
-            // p = 2^(x - m); c p as fp16, pairs of heads
+            // p = 2^(x - m), and the weights p c 2^(m - w) as fp16, pairs of heads
             const float m0 = m_run[0] == -INFINITY ? 0.f : m_run[0], m1 = m_run[1] == -INFINITY ? 0.f : m_run[1];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const float c = v_scale[u] * v_inv;
+                const float c0 = v_scale[u] * m_to_w[0], c1 = v_scale[u] * m_to_w[1];
                 uint32_t ph[2];
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     const float p0 = ex2_approx(x[u][2 * j] - m0), p1 = ex2_approx(x[u][2 * j + 1] - m1);
                     l_run[0] += p0;
                     l_run[1] += p1;
-                    ph[j] = pack_half(p0 * c, p1 * c);
+                    ph[j] = pack_half(p0 * c0, p1 * c1);
                 }
                 const uint32_t b0 = movmatrix_trans(ph[0]), b1 = movmatrix_trans(ph[1]);
                 // O^T += V^T (c P)^T
@@ -624,9 +644,9 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
             if (g == 0) {
                 sm.m[warp][2 * t + e] = m_run[e];
                 sm.l[warp][2 * t + e] = l_run[e];
+                sm.w[warp][2 * t + e] = w_run[e];
             }
         }
-        if (lane == 0) sm.vs[warp] = v_ref;
         for (int h0 = 0; h0 < G; h0 += 4) {
             if (2 * t >= h0 && 2 * t < h0 + 4)
 #pragma unroll
@@ -646,7 +666,8 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
                 float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
-                    const float wgt = sm.l[x][h] != 0.f ? exp2f(sm.m[x][h] - M) : 0.f, c = wgt * sm.vs[x];
+                    const float wgt = sm.l[x][h] != 0.f ? ex2_approx(sm.m[x][h] - M) : 0.f;
+                    const float c = sm.l[x][h] != 0.f ? ex2_approx(sm.w[x][h] - M) : 0.f;
                     const float4 y = *reinterpret_cast<const float4*>(&sm.o[x][h - h0][d]);
                     L += wgt * sm.l[x][h];
                     acc.x += c * y.x;

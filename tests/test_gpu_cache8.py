@@ -163,6 +163,47 @@ def test_decode_scales_of_any_size(kind):
 
 
 @pytest.mark.parametrize("kind", H8.KINDS)
+@pytest.mark.parametrize("block", [0, 3, 6])
+def test_small_values_beside_large_ones_of_little_weight(kind, block):
+    """One block has values 2^22 times as large as all others, and scores far below theirs: the weights of the small values keep
+    their precision.  With B the average of max|v_i|: weights as fp16 numbers are off by 2^-11 of themselves, or, where they are below
+    2^-14 of the largest one, by 2^-25 of that one, whose token has a code above a third of the largest (checked here): N tokens together by
+    (2^-11 + 3 N 2^-25) B.  Scores as in assert_attention, which gives 2^-15 (1 + A) B."""
+    import torch
+    c = H8.Case(kind, 4, 2, 64, [100, 112], style=2, seed=20 + block)
+    largest = 127 if kind == "int8" else 448
+    for score in (4.0, 9.0, 14.0, 16.0, 25.0):
+        q = H.synth.to_bf16_exact(np.repeat(c.rng.standard_normal((c.b, 1, c.H_kv, c.d_h)), c.G, axis=2)).astype(np.float64)
+        c.scales[0] = 2.0 ** -9 if kind == "int8" else 2.0 ** -11
+        c.scales[1] = 2.0 ** -24
+        for s in range(c.b):
+            for h in range(c.H_kv):
+                x = q[s, 0, h * c.G]
+                unit = C8.round_code(-x / np.abs(x).max() * largest, kind)
+                c.codes[0][s, 16 * block:16 * block + 16, h * c.d_h:(h + 1) * c.d_h] = unit
+                c.scales[0][s, block, h] = np.float32(score * np.sqrt(c.d_h) / -(unit @ x))
+                c.scales[1][s, block, h] = 2.0 ** -2
+        c.upload()
+        qd = H.dev_bf16(q)
+        out = torch.zeros(c.b, c.H_q, c.d_h, dtype=torch.bfloat16, device="cuda")
+        c.workspace()
+        c.L.lorc_decode_attn8(c.ctx, 0, c.cache(), qd, out)
+        got = H.host_f64(out)
+        want, size, _ = c.want(q)
+        for s, n in enumerate(c.lens):
+            k, v = c.held(0, s, n), c.held(1, s, n)
+            assert (np.abs(c.codes[1][s, :n].reshape(n, c.H_kv, c.d_h)).max(-1) > largest / 3).all()
+            for h in range(c.H_q):
+                x = k[:, h // c.G] @ q[s, 0, h] / np.sqrt(c.d_h)
+                w = np.exp(x - x.max())
+                B = (w * np.abs(v[:, h // c.G]).max(-1)).sum() / w.sum()
+                bound = 2.0 ** -8 * np.abs(want[s, 0, h]) + (2.0 ** -11 + 3 * n * 2.0 ** -25 + 2.0 ** -15 * (1 + size[s, 0, h])) * B
+                assert (np.abs(got[s, h] - want[s, 0, h]) <= bound).all(), (score, s, h)
+    assert c.status() == 0
+    c.close()
+
+
+@pytest.mark.parametrize("kind", H8.KINDS)
 @pytest.mark.parametrize("T", [1, 5])
 def test_rows_behind_the_end_are_not_read(kind, T):
     """Whatever stands behind a sequence's end: codes of NaN, scales that are NaN or infinite."""
