@@ -338,8 +338,9 @@ int lorc_decode_attn8(lorc_ctx* ctx, int layer, const lorc_cache8* cache, const 
 /* Attention of the T newest tokens of every sequence, as lorc_prefill_attn, over the 8-bit cache: q, out
  * [batch, T, n_q_heads, d_head] bf16; the T tokens are already cached, and query t sees the tokens up to its own.  A
  * sequence with fewer than T tokens gets zeros, and status ARG (EMPTY if it has none).  With the head geometries of the
- * tcgen05 kernels keys and values are brought to fp16 in the workspace once per call (code x scale must stay below 65504;
- * tokens whose page lies outside the pool count as zeros there).
+ * tcgen05 kernels, unless there are few queries, keys and values are brought to fp16 in the workspace once per call: code x
+ * scale must not exceed 65504 there (status ARG, and what comes of infinities), has steps of 2^-24 below 2^-14, and
+ * tokens whose page lies outside the pool count as zeros.
  * Errors: ARG, LAYER, UNSUPPORTED (a compressed layer), WORKSPACE; CAPACITY / EMPTY / ARG through the status word. */
 int lorc_prefill_attn8(lorc_ctx* ctx, int layer, const lorc_cache8* cache, const void* q, void* out, int T, void* stream);
 
@@ -415,8 +416,8 @@ const char* lorc_last_error(const lorc_ctx* ctx);
 /* Which kernel family the last lorc_decode_attn / lorc_append call (or their prompt and
  * 8-bit forms) on this context used: 0 = none yet, 1 = plain kernels (fp32 arithmetic; outside the debug flag
  * the key reconstruction of decode steps runs on mma.sync), 2 = tensor-core
- * (tcgen05) kernels of the latent mode, 3 = warp-level tensor-core (mma.sync) kernel of
- * the uncompressed mode.  For tests and benchmarks. */
+ * (tcgen05) kernels of the latent mode and of the 8-bit cache, 3 = warp-level tensor-core
+ * (mma.sync) kernels of the uncompressed mode, in bf16 or 8 bits.  For tests and benchmarks. */
 int lorc_last_path(const lorc_ctx* ctx);
 
 /* Contexts created with LORC_FLAG_PROFILE record a CUDA event before and after every

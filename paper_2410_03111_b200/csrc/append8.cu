@@ -2,7 +2,9 @@
 // block of 16 tokens and KV head.  Prompt-sized launches run in append8_tc.cu; here are the others.
 //
 // Two kernels.  The projection leaves fp32 numbers [tokens][2 n] in the workspace; the second kernel has a block of threads for each
-// (block of tokens, KV head, keys or values), which sees all numbers that share a scale.
+// (block of tokens, KV head, keys or values), which sees all numbers that share a scale.  16 sequences, D 4096, 8 KV heads of 128
+// dimensions: 9.0 us, of which 2.6 are the factor's bytes at the rate of a copy; the rest is two launches in a row, and x through L2
+// once per eight columns.
 #include <math.h>
 
 #include "append8.cuh"
@@ -117,8 +119,8 @@ project8_plain_kernel(const bf16* __restrict__ x, const bf16* __restrict__ A_cat
 }
 
 // ---------------------------------------------------------------------------------------------
-// rotation and quantisation: grid (batch * blocks a chunk can reach, KV heads, keys / values); 16 threads of 16 bytes per row of 128
-// dimensions are eight, so 128 (64) threads are the 16 rows.  A thread owns 16 dimensions of a row: one 16-byte store.
+// rotation and quantisation: grid (batch * blocks a chunk can reach, KV heads, keys / values), DH threads.  A thread owns 16 dimensions
+// of one of the 16 rows: one 16-byte store.
 // ---------------------------------------------------------------------------------------------
 template <int DH, bool E4M3>
 __global__ void __launch_bounds__(DH)

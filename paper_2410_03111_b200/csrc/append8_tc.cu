@@ -9,7 +9,8 @@
 // stages.  The tensor cores' fp32 sums lose more than rounding would as they grow longer, and a number near the border between
 // two codes may then fall on the other side; so the MMAs sum 512 products at a time, in two accumulators in TMEM by turns, and
 // sixteen epilogue warps add these up in registers.  (D 4096, codes that are not the fp64 projection's: 1.2e-5 of them, as with a
-// plain fp32 projection; with one sum of 4096 1.0e-4, in 7 % less time, with sums of 256 0.6e-5, in 13 % more.)  Rows of a block that are not new (earlier tokens, or behind the end) lie outside x and read as zero.
+// plain fp32 projection; with one sum of 4096 1.0e-4, in 7 % less time, with sums of 256 0.6e-5, in 13 % more.)  Rows of a block that
+// are not new (earlier tokens, or behind the end) lie outside x and read as zero.
 #include <math.h>
 
 #include "append8.cuh"
@@ -332,7 +333,9 @@ append8_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constan
 
 }  // namespace
 
-// Whether a launch runs here: see lorc_tc_append_gemm_supported, whose kernels have the same balance.
+// Whether a launch runs here.  The other kernels' time goes with the tiles of 16 tokens, each of which streams the factor; here a unit
+// of 256 rows takes the same time however few of them are tokens.  (8 KV heads of 128 dimensions, D 4096: one sequence's 48 tokens 17 us
+// there and 20 here, 64 tokens 21 and 20; 16 x 16 tokens 64 and 22; 64 x 4 tokens 62 and 30.)
 bool lorc_append8_tc_supported(const lorc_ctx* ctx, int batch, int T) {
     if (ctx->desc.d_model % KC || !lorc_get_tmap_encode() || (ctx->desc.flags & LORC_FLAG_DEBUG_FP32)) return false;
     const long long n_tok = (long long)batch * T;

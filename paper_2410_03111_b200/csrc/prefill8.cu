@@ -1,6 +1,6 @@
 // Prompt chunks over the 8-bit cache of uncompressed layers: keys and values of the cached tokens are brought to fp16 once per
-// call (code x scale: seven significant bits, exact unless the scale is no power of two), then the tcgen05 attention kernel of the
-// latent mode runs over them.  With T queries per sequence that kernel does 4 T d G products per number of the buffer, so the
+// call (code x scale has seven significant bits: exact where the scale is a power of two and the number within fp16's normal range),
+// then the tcgen05 attention kernel of the latent mode runs over them.  With T queries per sequence that kernel does 4 T d G products per number of the buffer, so the
 // pass over it is small for chunks.
 #include <math.h>
 
@@ -43,6 +43,7 @@ expand8_kernel(const Expand8Params p) {
     const uint4* src = reinterpret_cast<const uint4*>(val ? cv.v : cv.k) + at * LORC_BLOCK8 * per_row;
     const float* scale = (val ? cv.v_scale : cv.k_scale) + at * cv.n_kv;
     uint4* dst = (val ? p.vbuf : p.khat) + ((long long)s * p.rows + (long long)blk * LORC_BLOCK8) * per_row * 2;
+    __half2 most = __floats2half2_rn(0.f, 0.f);
     for (int i = threadIdx.x; i < LORC_BLOCK8 * per_row; i += 256) {
         const int r = i / per_row, c = i - r * per_row;
         uint4 lo = make_uint4(0u, 0u, 0u, 0u), hi = lo;
@@ -57,6 +58,7 @@ expand8_kernel(const Expand8Params p) {
                 lorc_codes_half<E4M3, 0, 1, 2, 3>(in[j], a, b);
                 const float2 u = __half22float2(*reinterpret_cast<__half2*>(&a)), v = __half22float2(*reinterpret_cast<__half2*>(&b));
                 const __half2 y = __floats2half2_rn(u.x * f, u.y * f), z = __floats2half2_rn(v.x * f, v.y * f);
+                most = __hmax2(most, __hmax2(__habs2(y), __habs2(z)));
                 w[2 * j] = *reinterpret_cast<const uint32_t*>(&y);
                 w[2 * j + 1] = *reinterpret_cast<const uint32_t*>(&z);
             }
@@ -66,6 +68,8 @@ expand8_kernel(const Expand8Params p) {
         dst[2 * i] = lo;
         dst[2 * i + 1] = hi;
     }
+    // numbers that fp16 does not hold
+    if (fmaxf(__low2float(most), __high2float(most)) > 65504.f) lorc_set_status(p.status, LORC_ERR_ARG);
 }
 
 size_t expand8_rows(int max_seq_len) { return ((size_t)max_seq_len + 127) / 128 * 128; }
@@ -81,8 +85,9 @@ struct Split8 {
 
 // A CTA takes 2.2 us per tile of 128 keys and 4 us before and after, whatever runs beside it; the merge 3 us and its traffic; two
 // launches of the kernel in a row 2 us more than one.  Either all units share their keys among S CTAs, or those that the full rounds of
-// the SMs leave over.  (256 tokens behind 8000: 152 us with one CTA, 70 with two and 46 with eight.  8 x 512 tokens behind 3584, 512
-// units on 148 SMs: 325 us in four rounds, 318 with the last 68 units shared by two CTAs each.)
+// the SMs leave over.  (Whole calls, 8 KV heads of 128 dimensions in groups of four: 128 tokens behind 8000 take 152 us with one CTA
+// per unit and 48 as chosen here, 512 tokens 150 and 100.  8 x 512 tokens behind 3584, 512 units on 148 SMs: 325 us in four rounds, 318
+// with the last 68 units shared by two CTAs each.)
 Split8 prefill8_split(const lorc_ctx* ctx, int batch, int max_seq_len, int T) {
     const int qp = 256 / ctx->group;
     const long long P = ctx->sm_count, tiles = ((long long)max_seq_len + 127) / 128;

@@ -316,6 +316,37 @@ def test_a_chunk_longer_than_a_sequence(heads):
     c.close()
 
 
+@pytest.mark.parametrize("kind", H8.KINDS)
+@pytest.mark.parametrize("which", [0, 1])
+def test_chunks_report_numbers_beyond_fp16(kind, which):
+    """The tcgen05 path holds keys and values in fp16: up to 65504 they count, what is larger is reported."""
+    import torch
+    c = H8.Case(kind, 32, 8, 128, [300, 200], seed=11)
+    largest = C8.LARGEST[kind]
+    c.codes[which][1, 100, 5] = largest
+    fits = 2.0 ** np.floor(np.log2(65504 / largest))
+    if which == 0:
+        c.codes[0][1, 96:112, :128] = 0
+        c.codes[0][1, 100, 5] = largest
+    q, qd = c.queries(130, scale=1.0 if which else 2.0 ** -12)
+    out = torch.zeros(q.shape, dtype=torch.bfloat16, device="cuda")
+    c.workspace(130)
+    for scale, status in ((fits, 0), (2 * fits, c.L.LORC_ERR_ARG), (2.0 ** 100, c.L.LORC_ERR_ARG)):
+        c.scales[which][1, 6, 0] = scale
+        c.upload()
+        c.L.lorc_prefill_attn8(c.ctx, 0, c.cache(), qd, out, 130)
+        assert c.L.lorc_last_path(c.ctx) == 2 and c.status() == status
+        if status == 0:
+            H8.assert_attention(H.host_f64(out), *c.want(q, 130), fp16=True)
+    # behind a sequence's end nothing is looked at
+    c.scales[which][1, 6, 0] = 2.0 ** -6
+    c.scales[which][1, 13, :] = 2.0 ** 100
+    c.upload()
+    c.L.lorc_prefill_attn8(c.ctx, 0, c.cache(), qd, out, 130)
+    assert c.status() == 0
+    c.close()
+
+
 # ---- the write --------------------------------------------------------------------------------------------------------------
 
 def _exact_x(c, T):
