@@ -271,7 +271,7 @@ append8_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constan
                 __syncwarp();
                 if (lane == 0) mbar_arrive_cluster(lead_acc_empty[buf]);      // this warp has read its part of the accumulator
             }
-            // rotation, and the largest magnitudes; -1 stands for a number that is not finite
+            // rotation, and the largest magnitudes; a sign bit stands for a number that is not finite (and does not count)
             float most[NP], before[NP];
             // (rows that are not to be written are rotated as position 0; their numbers are zero)
             const float4* far = reinterpret_cast<const float4*>(p.q.rope_table + (long long)(row.pos & ~(LORC_BLOCK8 - 1)) * (DH / 2));
@@ -282,7 +282,7 @@ append8_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constan
                 if (!val && ok) append8_rotate(c, il, far, near, a[k], b[k]);
                 bool odd = false;
                 most[k] = fmaxf(append8_most(a[k], odd), append8_most(b[k], odd));
-                if (odd && row.fresh) most[k] = -1.f;
+                if (odd && row.fresh) most[k] = -most[k];
                 sm.most[turn][k][group][quarter * 32 + lane] = most[k];
                 before[k] = row.at >= 0 && row.has_old ? (val ? cv.v_scale : cv.k_scale)[row.at * cv.n_kv + (val ? head - cv.n_kv : head)] : 0.f;
             }
@@ -292,14 +292,14 @@ append8_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constan
             for (int k = 0; k < NP; ++k) {
                 const int head = col0 / DH + (k * 4 + group) / PIECES, h = head >= cv.n_kv ? head - cv.n_kv : head;
                 const bool val = head >= cv.n_kv;
-                bool odd = most[k] < 0.f;
+                bool odd = signbit(most[k]);
+                most[k] = fabsf(most[k]);
 #pragma unroll
                 for (int x = 1; x < SHARE; ++x) {
                     const float other = sm.most[turn][k][group / SHARE * SHARE + (group + x) % SHARE][quarter * 32 + lane];
-                    odd |= other < 0.f;
-                    most[k] = fmaxf(most[k], other);
+                    odd |= signbit(other);
+                    most[k] = fmaxf(most[k], fabsf(other));
                 }
-                most[k] = fmaxf(most[k], 0.f);
 #pragma unroll
                 for (int o = 1; o < 16; o <<= 1) most[k] = fmaxf(most[k], __shfl_xor_sync(0xffffffffu, most[k], o));
                 const bool any_odd = __ballot_sync(0xffffffffu, odd) >> (lane & 16) & 0xffff;
@@ -334,8 +334,8 @@ append8_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constan
 }  // namespace
 
 // Whether a launch runs here.  The other kernels' time goes with the tiles of 16 tokens, each of which streams the factor; here a unit
-// of 256 rows takes the same time however few of them are tokens.  (8 KV heads of 128 dimensions, D 4096: one sequence's 48 tokens 17 us
-// there and 20 here, 64 tokens 21 and 20; 16 x 16 tokens 64 and 22; 64 x 4 tokens 62 and 30.)
+// of 256 rows takes the same time however few of them are tokens.  (8 KV heads of 128 dimensions, D 4096, us there and here: one
+// sequence's 48 tokens 17 and 21, 64 tokens 21 and 21; 64 x 1 tokens 22 and 22, 200 x 1 64 and 54, 16 x 16 61 and 22, 64 x 4 62 and 32.)
 bool lorc_append8_tc_supported(const lorc_ctx* ctx, int batch, int T) {
     if (ctx->desc.d_model % KC || !lorc_get_tmap_encode() || (ctx->desc.flags & LORC_FLAG_DEBUG_FP32)) return false;
     const long long n_tok = (long long)batch * T;

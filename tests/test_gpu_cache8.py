@@ -427,6 +427,18 @@ def test_write_of_gaussian_tokens(kind, style, heads, D, T, lens):
 
 
 @pytest.mark.parametrize("kind", H8.KINDS)
+@pytest.mark.parametrize("style", [0, 1])
+@pytest.mark.parametrize("heads,D", [((4, 2, 64), 512), ((3, 3, 128), 5120), ((7, 1, 64), 8192)])
+@pytest.mark.parametrize("b", [1, 16, 37])
+def test_write_of_single_tokens(kind, style, heads, D, b):
+    """One token per sequence, at every place of a block: as gaussian tokens, and exactly."""
+    lens = [1 + (29 * s) % 67 for s in range(b)]
+    test_write_of_gaussian_tokens(kind, style, heads, D, 1, lens)
+    if style == 0:
+        test_write_is_exact_where_the_projection_is(kind, heads, D, 1, lens, 16)
+
+
+@pytest.mark.parametrize("kind", H8.KINDS)
 def test_numbers_that_are_not_finite(kind):
     """They are reported and contained: NaN becomes 0, an infinity the largest code, other heads and blocks are as ever."""
     import torch
@@ -444,6 +456,44 @@ def test_numbers_that_are_not_finite(kind):
     top = C8.LARGEST[kind]
     assert (got[1, 0, 38:40, 3] == top).all() and (got[1, 0, 38:40, 5] == 0).all()
     assert np.isfinite(got).all() and bool(torch.isfinite(c.sc).all())
+    c.close()
+
+
+@pytest.mark.parametrize("kind", H8.KINDS)
+@pytest.mark.parametrize("T,lens", [(1, [17, 40]), (2, [40]), (100, [140])])
+def test_finite_numbers_beside_others_count_for_the_scale(kind, T, lens):
+    """The largest finite numbers of a block stand next to a NaN and an infinity: codes and scales are the oracle's."""
+    c = H8.Case(kind, 8, 8, 128, lens, D=512, style=H.ROPE_NONE, seed=T + 30)
+    w = np.asarray(c.w[1]).copy()
+    w[:, :16] = w[:, :16] * 16
+    bad = w.copy()
+    bad[7, 3], bad[7, 5] = np.inf, np.nan
+    c.L.lorc_load_factors(c.ctx, 0, c.L.LORC_MODE_FULL, 0, 0, H.dev_bf16(c.w[0]), None, H.dev_bf16(bad), None)
+    c.w[1] = w
+    at, _ = _exact_x(c, T)
+    at[:, -1] = 7
+    x = np.zeros((c.b, T, c.D))
+    x[np.arange(c.b)[:, None], np.arange(T), at] = 1.0
+    want_codes, want_scales = c.codes.copy(), c.scales.copy()
+    for s, n in enumerate(c.lens):
+        page, row = c.rows_of(s, -(-n // 16) * 16)
+        for i in range(2):
+            new = np.asarray(c.w[i], dtype=np.float64)[at[s]]
+            if i == 1:
+                new[:, [3, 5]] = 0.0
+            codes = want_codes[i][page, row].reshape(-1, c.H_kv, c.d_h)
+            scales = want_scales[i][page[::16], row[::16] // 16]
+            C8.write(codes, scales, new.reshape(T, c.H_kv, c.d_h), n, kind)
+            want_codes[i][page, row] = codes.reshape(-1, c.n)
+            want_scales[i][page[::16], row[::16] // 16] = scales
+            if i == 1:
+                want_codes[1][s, n - T:n, 3] = np.where(at[s] == 7, C8.LARGEST[kind], 0.0)     # (0 x inf is NaN)
+    c.workspace(T)
+    c.L.lorc_append8(c.ctx, 0, c.cache(), H.dev_bf16(x), T)
+    assert c.status() == c.L.LORC_ERR_ARG
+    assert c.L.lorc_last_path(c.ctx) == (2 if T == 100 else 3)
+    assert np.array_equal(c.sc.double().cpu().numpy(), want_scales)
+    assert np.array_equal(H8.host_codes(c.kv, kind), want_codes)
     c.close()
 
 
