@@ -208,7 +208,8 @@ __device__ __forceinline__ D8Range d8_range(const D8Params& p, int part, int lan
 #pragma unroll
     for (int c = 0; c < 4; ++c)
         if (!found && c * 32 < p.rows) look(c * 32, w[c]);
-    for (int i0 = 128; !found; i0 += 32) look(i0, i0 + lane < p.rows ? d8_weight(d8_len(p, i0 + lane, nullptr)) : 0);
+    for (int i0 = 128; !found && i0 < p.rows; i0 += 32) look(i0, i0 + lane < p.rows ? d8_weight(d8_len(p, i0 + lane, nullptr)) : 0);
+    if (!found) r.end = r.f;                     // (lengths that change under way)
     return r;
 }
 
