@@ -321,12 +321,12 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
                     first += w;
                     ++row;
                 }
-                for (; f < range.end; ++row) {
+                for (; f < range.end && row < p.rows; ++row) {
                     len = d8_len(p, row, nullptr);
                     if (len > 0) break;
                     f = ++first;
                 }
-                if (f >= range.end) {
+                if (f >= range.end || row >= p.rows) {
                     more = false;
                     return;
                 }
@@ -414,7 +414,7 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
         // ------------------------------------------------------------------ queries: RoPE(q, position) of the G heads, one row ahead
         constexpr int E = DH / 64;               // rotary pairs per lane
         int f = range.f, first = range.first;
-        for (int row = range.row; f < range.end && ok; ++row) {
+        for (int row = range.row; f < range.end && row < p.rows && ok; ++row) {
             const int len = d8_len(p, row, nullptr), w = d8_weight(len);
             if (len > 0) {
                 const bf16* q = p.q + ((long long)row * H_q + kvh * G) * DH;
@@ -468,7 +468,7 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
     const uint32_t row_off = my_row * DH, sw = DH == 128 ? my_row & 7 : (my_row >> 1) & 3;
     uint32_t q_par = 0;
     int f = range.f, first = range.first;
-    for (int row = range.row; f < range.end; ++row) {
+    for (int row = range.row; f < range.end && row < p.rows; ++row) {
         const int len = d8_len(p, row, tid == 0 ? p.status : nullptr), w = d8_weight(len);
         const int stop = min(first + w, range.end);
         const bool whole = f == first && stop == first + w;
