@@ -1,4 +1,4 @@
-// Attention over the 8-bit cache of uncompressed layers, one query per sequence and head, on the warp-level tensor cores.
+// Attention over the 8-bit cache of uncompressed layers, one or few queries per sequence, on the warp-level tensor cores.
 //
 // One pass over 2 n bytes per token, bound by HBM: a block streams (sequence, KV head) pairs; a producer warp keeps D8_STAGES
 // 128-token stages of codes in flight by TMA, and each of four consumer warps takes 32 of a stage's tokens, two blocks of the cache
@@ -23,6 +23,10 @@
 // a sequence; what it computes of a sequence that it does not hold alone goes to memory, un-normalised, and the last of the
 // sequence's parts to get there adds them up.  (A merge kernel of its own cost 6 to 8 us more; the same by the queries' warp, so that
 // the others go on, 1 to 3 us more, since one warp takes longer over it at the end of the launch.)
+//
+// Several queries of a sequence (prompt chunks of few tokens, drafts that are verified) are rows of as many queries as fit the eight
+// columns; each column has its own last token.  (8 x 4096 tokens, four heads per KV head: 4 queries 31 us, one by one 43; 16
+// queries 90 and 147.)
 //
 // Measured, 8 KV heads of 128 dimensions: 16 x 4129 tokens 30 us (4.5 TB/s), 4 x 32777 49 us (5.5), 64 sequences of 512 to
 // 16384 185 us (6.0; a copy 6.6), 128 x 300 31 us: there it is the 1.5 us per sequence and block from its last tile's
@@ -108,8 +112,9 @@ struct D8Params {
     unsigned* count;                            // [n_kv][parts], zero between calls
     int* status;
     int G, n_kv, T, interleaved, max_pos, box_rows;
+    int Q, per_seq, cols;                       // queries of a sequence that share a row, rows per sequence, G * Q
     unsigned page_magic;                        // see d8_page_of
-    int rows;                                   // batch * T
+    int rows;                                   // batch * per_seq
     int each;                                   // parts / rows, where a list has at most 128 rows
     int parts, least;                           // 0: a block per row and KV head; else parts of the list, of `least` steps at least
 };
@@ -123,15 +128,17 @@ __device__ __forceinline__ int d8_page_of(const D8Params& p, int b) {
     return q * per > b ? q - 1 : q;
 }
 
-// Row r = s T + t stands for query t of sequence s: the tokens up to that query's own (0: nothing to attend to).
+// Row r = s per_seq + j stands for the queries j Q .. j Q + Q - 1 of sequence s (the last row may have fewer): the tokens up to the
+// last one's own (0: nothing to attend to).
+__device__ __forceinline__ int d8_queries(const D8Params& p, int j) { return min(p.Q, p.T - j * p.Q); }
 __device__ __forceinline__ int d8_len(const D8Params& p, int r, int* status) {
     if (p.T == 1) return lorc_len8(p.cv, r, p.max_pos, status);
-    const int s = r / p.T, len = lorc_len8(p.cv, s, p.max_pos, status);
+    const int s = r / p.per_seq, len = lorc_len8(p.cv, s, p.max_pos, status);
     if (len < p.T) {
         if (len > 0 && status) lorc_set_status(status, LORC_ERR_ARG);
         return 0;
     }
-    return len - (p.T - 1 - (r - s * p.T));
+    return len - max(p.T - (r - s * p.per_seq + 1) * p.Q, 0);
 }
 // Units of a row on the list; a row without tokens has one, in which its zeros are written.
 __device__ __forceinline__ int d8_weight(int len) { return len <= 0 ? 1 : (len - 1) / D8_UNIT + 1; }
@@ -221,11 +228,21 @@ __device__ __forceinline__ void d8_store(const D8Params& p, long long at, const 
     if (L == 0.f) lorc_set_status(p.status, LORC_ERR_EMPTY);
 }
 
-// Merge of a row that was cut into n pieces: the G heads of a KV head, by 128 threads, four dimensions each.  Pieces come four at a
+// Where column h of a row goes: head h of the KV head, or head h % G of query h / G.
+template <bool MULTI>
+__device__ __forceinline__ long long d8_out_row(const D8Params& p, int row, int kvh, int h) {
+    const int H_q = p.G * p.n_kv;
+    if (!MULTI) return (long long)row * H_q + kvh * p.G + h;
+    const int s = row / p.per_seq, t = (row - s * p.per_seq) * p.Q + h / p.G;
+    return ((long long)s * p.T + t) * H_q + kvh * p.G + h % p.G;
+}
+
+// Merge of a row that was cut into n pieces: the `cols` columns of a KV head, by 128 threads, four dimensions each.  Pieces come four at a
 // time, and the sums so far are brought to a new reference with each four: one round trip to L2 per four pieces.
-template <int DH>
-__device__ __forceinline__ void d8_merge(const D8Params& p, long long unit0, int n, long long out0, int tid) {
-    for (int i = tid; i < p.G * (DH / 4); i += 128) {
+template <int DH, bool MULTI>
+__device__ __forceinline__ void d8_merge(const D8Params& p, long long unit0, int n, int row, int kvh, int cols, int tid) {
+    const int stride = MULTI ? p.cols : p.G;
+    for (int i = tid; i < cols * (DH / 4); i += 128) {
         const int h = i / (DH / 4), d = (i - h * (DH / 4)) * 4;
         const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + unit0 + h;
         const float* po = p.part_o + (unit0 + h) * DH + d;
@@ -239,8 +256,8 @@ __device__ __forceinline__ void d8_merge(const D8Params& p, long long unit0, int
                 x[c] = make_float2(0.f, 0.f);
                 y[c] = make_float4(0.f, 0.f, 0.f, 0.f);
                 if (c0 + c < n) {
-                    x[c] = __ldcg(ml + (long long)(c0 + c) * p.G);
-                    y[c] = __ldcg(reinterpret_cast<const float4*>(po + (long long)(c0 + c) * p.G * DH));
+                    x[c] = __ldcg(ml + (long long)(c0 + c) * stride);
+                    y[c] = __ldcg(reinterpret_cast<const float4*>(po + (long long)(c0 + c) * stride * DH));
                 }
             }
             float now = M;
@@ -264,11 +281,12 @@ __device__ __forceinline__ void d8_merge(const D8Params& p, long long unit0, int
                 acc.w += wgt * y[c].w;
             }
         }
-        d8_store(p, (out0 + h) * DH + d, acc, L);
+        d8_store(p, d8_out_row<MULTI>(p, row, kvh, h) * DH + d, acc, L);
     }
 }
 
-template <int DH, bool E4M3>
+// MULTI: rows of several queries.
+template <int DH, bool E4M3, bool MULTI>
 __global__ void __launch_bounds__(D8_THREADS, D8_BLOCKS_PER_SM)
 decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV, const D8Params p) {
     constexpr int KS = DH / 16;                  // pieces of 16 dimensions
@@ -278,7 +296,7 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
     const int g = lane >> 2, t = lane & 3;       // fragment row / column group of this lane
     const int kvh = (int)blockIdx.x % p.n_kv, part = (int)blockIdx.x / p.n_kv;
     const Cache8View& cv = p.cv;
-    const int G = p.G, H_q = G * p.n_kv;
+    const int G = p.G;
     if (tid == 0) {
         for (int i = 0; i < D8_STAGES; ++i) {
             mbar_init(&sm.full[i], 2);           // the copies, and the scales
@@ -330,7 +348,7 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
                     more = false;
                     return;
                 }
-                next.s = p.T == 1 ? row : row / p.T;
+                next.s = p.T == 1 ? row : row / p.per_seq;
                 next.t0 = (f - first) * D8_UNIT;
                 next.t_end = min(len, (min(first + d8_weight(len), range.end) - first) * D8_UNIT);
             }
@@ -411,14 +429,14 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
         return;
     }
     if (warp == 5) {
-        // ------------------------------------------------------------------ queries: RoPE(q, position) of the G heads, one row ahead
+        // ------------------------------------------------------------------ queries: RoPE(q, position) of the row's columns, one row ahead
         constexpr int E = DH / 64;               // rotary pairs per lane
         int f = range.f, first = range.first;
         for (int row = range.row; f < range.end && row < p.rows && ok; ++row) {
             const int len = d8_len(p, row, nullptr), w = d8_weight(len);
             if (len > 0) {
-                const bf16* q = p.q + ((long long)row * H_q + kvh * G) * DH;
-                const float2* cs = p.rope_table + (long long)(len - 1) * (DH / 2) + lane * E;
+                const int nq = MULTI ? d8_queries(p, row % p.per_seq) : 1, cols = nq * G;
+                const float2* cs = p.rope_table + (long long)(len - nq) * (DH / 2) + lane * E;      // of the first query
                 int ia[E], ib[E];
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
@@ -426,19 +444,23 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
                     ib[e] = p.interleaved ? ia[e] + 1 : ia[e] + DH / 2;
                 }
                 bf16 a[8][E], b[8][E];
-                float2 c[E];
+                float2 c[MULTI ? 8 : 1][E];
 #pragma unroll
-                for (int h = 0; h < 8; ++h)
+                for (int h = 0; h < 8; ++h) {
+                    const bf16* q = p.q + d8_out_row<MULTI>(p, row, kvh, h) * DH;
 #pragma unroll
                     for (int e = 0; e < E; ++e) {
                         a[h][e] = b[h][e] = __float2bfloat16_rn(0.f);
-                        if (h < G) {
-                            a[h][e] = q[h * DH + ia[e]];
-                            b[h][e] = q[h * DH + ib[e]];
+                        if (h < cols) {
+                            a[h][e] = q[ia[e]];
+                            b[h][e] = q[ib[e]];
                         }
+                        if (MULTI) c[MULTI ? h : 0][e] = h < cols ? cs[(long long)(h / G) * (DH / 2) + e] : make_float2(0.f, 0.f);
                     }
+                }
+                if (!MULTI)
 #pragma unroll
-                for (int e = 0; e < E; ++e) c[e] = cs[e];
+                    for (int e = 0; e < E; ++e) c[0][e] = cs[e];
                 ok = __all_sync(0xffffffffu, mbar_wait(&sm.q_empty, par ^ 1));
                 if (!ok) break;
 #pragma unroll
@@ -446,8 +468,9 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
 #pragma unroll
                     for (int e = 0; e < E; ++e) {
                         const float x = __bfloat162float(a[h][e]), y = __bfloat162float(b[h][e]);
-                        sm.qs[h][ia[e]] = x * c[e].x - y * c[e].y;
-                        sm.qs[h][ib[e]] = x * c[e].y + y * c[e].x;
+                        const float2 w = c[MULTI ? h : 0][e];
+                        sm.qs[h][ia[e]] = x * w.x - y * w.y;
+                        sm.qs[h][ib[e]] = x * w.y + y * w.x;
                     }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sm.q_full);
@@ -473,6 +496,14 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
         const int stop = min(first + w, range.end);
         const bool whole = f == first && stop == first + w;
         const int t_begin = (f - first) * D8_UNIT, t_end = min(len, (stop - first) * D8_UNIT);
+        const int nq = MULTI ? d8_queries(p, row % p.per_seq) : 1, cols = nq * G;
+        // (of a row of several queries, heads 2 t, 2 t + 1 of the first ones see fewer tokens)
+        int seen[2] = {t_end, t_end}, seen_least = t_end;
+        if (MULTI) {
+            seen_least = min(t_end, len - (nq - 1));
+#pragma unroll
+            for (int e = 0; e < 2; ++e) seen[e] = min(t_end, len - max(nq - 1 - (2 * t + e) / G, 0));
+        }
 
         if (len > 0) {
             if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&sm.q_full, q_par));
@@ -549,14 +580,14 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
                 for (int j = 0; j < 4; ++j) x[u][j] = (sc[0][j] + sc[1][j]) * (j & 1 ? f1 : f0);
             }
             const uint32_t dead = sm.dead[st];
-            if (tw + 32 > t_end || dead) {       // tokens past the end, or in pages that do not exist
+            if (tw + 32 > seen_least || dead) {  // tokens past the end, or in pages that do not exist
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    const int live = (dead >> (2 * warp + u)) & 1 ? 0 : t_end - tw - 16 * u;
-                    if (live <= 0) v_scale[u] = 0.f;
+                    const bool gone = (dead >> (2 * warp + u)) & 1;
+                    if (gone || t_end - tw - 16 * u <= 0) v_scale[u] = 0.f;
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
-                        if (g + (j >> 1) * 8 >= live) x[u][j] = -INFINITY;
+                        if (gone || g + (j >> 1) * 8 >= seen[j & 1] - tw - 16 * u) x[u][j] = -INFINITY;
                 }
                 if (E4M3) {
                     // such rows have the factor zero, but their bytes may be codes of NaN
@@ -648,7 +679,7 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
                 sm.w[warp][2 * t + e] = w_run[e];
             }
         }
-        for (int h0 = 0; h0 < G; h0 += 4) {
+        for (int h0 = 0; h0 < cols; h0 += 4) {
             if (2 * t >= h0 && 2 * t < h0 + 4)
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
@@ -658,7 +689,7 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
             __syncwarp();
             asm volatile("bar.sync 1, 128;" ::: "memory");
             const int h = h0 + tid / (DH / 4), d = tid % (DH / 4) * 4;          // a thread takes four dimensions of a head
-            if (h < min(G, h0 + 4)) {
+            if (h < min(cols, h0 + 4)) {
                 float M = -INFINITY;
 #pragma unroll
                 for (int x = 0; x < 4; ++x)
@@ -677,9 +708,9 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
                     acc.w += c * y.w;
                 }
                 if (whole) {
-                    d8_store(p, ((long long)row * H_q + kvh * G + h) * DH + d, acc, L);
+                    d8_store(p, d8_out_row<MULTI>(p, row, kvh, h) * DH + d, acc, L);
                 } else {
-                    const long long unit = ((long long)kvh * (p.parts + p.rows) + part + row) * G + h;
+                    const long long unit = ((long long)kvh * (p.parts + p.rows) + part + row) * (MULTI ? p.cols : G) + h;
                     if (d == 0) *reinterpret_cast<float2*>(p.part_ml + unit * 2) = make_float2(M, L);
                     *reinterpret_cast<float4*>(p.part_o + unit * DH + d) = acc;
                 }
@@ -697,7 +728,7 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
             asm volatile("bar.sync 1, 128;" ::: "memory");
             if (sm.last) {
                 __threadfence();
-                d8_merge<DH>(p, ((long long)kvh * (p.parts + p.rows) + c0 + row) * G, n, (long long)row * H_q + kvh * G, tid);
+                d8_merge<DH, MULTI>(p, ((long long)kvh * (p.parts + p.rows) + c0 + row) * (MULTI ? p.cols : G), n, row, kvh, cols, tid);
             }
         }
         first += w;
@@ -733,30 +764,38 @@ size_t d8_ml_bytes(const lorc_ctx* ctx, long long slots) {
     return lorc_align_up((size_t)slots * ctx->desc.n_q_heads * 2 * sizeof(float), 256);
 }
 
-template <int DH, bool E4M3>
+template <int DH, bool E4M3, bool MULTI>
 cudaError_t d8_launch(lorc_ctx* ctx, const CUtensorMap& mapK, const CUtensorMap& mapV, const D8Params& p, cudaStream_t st) {
     const size_t smem = sizeof(D8Smem<DH>) + 1024;
     // the attribute belongs to a device's copy of the kernel: one flag per device
     static bool attr[64] = {false};
     const bool known = ctx->device >= 0 && ctx->device < 64;
     if (!known || !attr[ctx->device]) {
-        cudaError_t e = cudaFuncSetAttribute(decode8_mma_kernel<DH, E4M3>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        cudaError_t e = cudaFuncSetAttribute(decode8_mma_kernel<DH, E4M3, MULTI>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
         if (known) attr[ctx->device] = true;
     }
     const long long blocks = (long long)p.n_kv * (p.parts ? p.parts : p.rows);
     if (blocks > 0x7fffffffll) return cudaErrorInvalidValue;
-    return lorc_launch_dependent(decode8_mma_kernel<DH, E4M3>, dim3((unsigned)blocks), dim3(D8_THREADS), smem, st, mapK, mapV, p);
+    return lorc_launch_dependent(decode8_mma_kernel<DH, E4M3, MULTI>, dim3((unsigned)blocks), dim3(D8_THREADS), smem, st, mapK, mapV, p);
+}
+
+template <int DH, bool E4M3>
+cudaError_t d8_launch(lorc_ctx* ctx, const CUtensorMap& mapK, const CUtensorMap& mapV, const D8Params& p, cudaStream_t st) {
+    return p.Q > 1 ? d8_launch<DH, E4M3, true>(ctx, mapK, mapV, p, st) : d8_launch<DH, E4M3, false>(ctx, mapK, mapV, p, st);
 }
 
 }  // namespace
 
+int lorc_decode8_queries(const lorc_ctx* ctx, int T) { return T < 8 / ctx->group ? T : 8 / ctx->group; }
+
 size_t lorc_decode8_scratch_bytes(const lorc_ctx* ctx, int batch, int max_seq_len, int T) {
-    // a call may have fewer tokens or shorter sequences than stated here: room for the list in any case
+    // a call may have fewer queries or shorter sequences than stated here: room for the list in any case (one query: all sequences
+    // are on it; several: fewer rows than there are parts, of Q queries each)
     int parts, least;
-    const long long rows = (long long)batch * T;
     d8_plan(ctx, 1, max_seq_len > 4 * D8_UNIT ? max_seq_len : 4 * D8_UNIT + 1, 1, &parts, &least);
-    const long long slots = parts + (batch > parts || rows <= batch ? batch : rows < parts ? rows : parts);
+    const long long Q = lorc_decode8_queries(ctx, T), one = (long long)parts + batch, several = T > 1 ? 2ll * parts * Q : 0;
+    const long long slots = one > several ? one : several;
     return d8_ml_bytes(ctx, slots) + lorc_align_up((size_t)slots * ctx->desc.n_q_heads * ctx->desc.d_head * sizeof(float), 256);
 }
 
@@ -771,13 +810,17 @@ cudaError_t lorc_decode8_launch(lorc_ctx* ctx, const Cache8View& cv, const bf16*
     p.q = q; p.out = out; p.cv = cv; p.rope_table = ctx->rope_table; p.status = ctx->status_dev;
     p.count = ctx->part_count;
     p.G = ctx->group; p.n_kv = d.n_kv_heads; p.T = T; p.interleaved = ctx->pair_style == LORC_ROPE_INTERLEAVED;
-    p.max_pos = d.max_pos; p.box_rows = box_rows; p.rows = cv.batch * T;
+    p.max_pos = d.max_pos; p.box_rows = box_rows;
+    p.Q = lorc_decode8_queries(ctx, T);
+    p.per_seq = (T + p.Q - 1) / p.Q;
+    p.cols = p.Q * p.G;
+    p.rows = cv.batch * p.per_seq;
     const unsigned per = cv.page_table ? cv.page_size / LORC_BLOCK8 : 1;
     p.page_magic = per > 1 ? (unsigned)(((1ull << 32) + per - 1) / per) : 0;
     d8_plan(ctx, p.rows, cv.max_seq_len, T, &p.parts, &p.least);
     p.each = p.rows <= 128 ? p.parts / p.rows : 0;
     p.part_ml = (float*)scratch;
-    p.part_o = (float*)((char*)scratch + d8_ml_bytes(ctx, p.parts + p.rows));
+    p.part_o = (float*)((char*)scratch + d8_ml_bytes(ctx, (long long)(p.parts + p.rows) * p.Q));
     const bool e4m3 = cv.type == LORC_CACHE8_E4M3;
     LorcStageTimer timer(ctx, LORC_STAGE_SCORE, st);
     *launches += 1;

@@ -117,13 +117,15 @@ size_t expand8_bytes(const lorc_ctx* ctx, int batch, int max_seq_len) {
 
 }  // namespace
 
-// Few queries per sequence are better served by the streaming kernel, which reads the codes once per query (from L2, mostly) and is
-// then bound by its arithmetic: 0.33 us per 64 tokens, query and KV head on an SM, against 1.3 us to expand them for all queries (8 x 4096
-// tokens, 8B shape, 4 queries 43 us against 112, 16 queries 147 against 108; one sequence of 1000 tokens, 32 queries 16 against 26).
+// Few queries per sequence are better served by the streaming kernel, which reads the codes once per lorc_decode8_queries of them (from
+// L2, mostly) and is then bound by its arithmetic: 0.33 us per 64 tokens, pass and KV head on an SM, against 1.3 us to expand them for
+// all queries.  (8 KV heads of 128 dimensions in groups of four, us here and there: 8 x 4096 tokens, 4 queries 31 and 87, 16 queries
+// 90 and 87, 32 queries 161 and 89; one sequence of 1000 tokens, 32 queries 15 and 20; of 8000, 32 queries 49 and 41.)
 bool lorc_prefill8_supported(const lorc_ctx* ctx, const Cache8View& cv, int T) {
     if (T == 1 || cv.batch > 65535 || !lorc_tc_prefill_shape_ok(ctx) || (ctx->desc.flags & LORC_FLAG_DEBUG_FP32)) return false;
     const long long units = (long long)cv.batch * cv.n_kv * ((cv.max_seq_len + 63) / 64), P = ctx->sm_count;
-    const long long stream = 80 + 33 * units * T / (10 * P);
+    const int Q = lorc_decode8_queries(ctx, T);
+    const long long stream = 80 + 33 * units * ((T + Q - 1) / Q) / (10 * P);
     const long long expand = 100 + 13 * units / P + prefill8_split(ctx, cv.batch, cv.max_seq_len, T).time;
     return expand < stream;
 }

@@ -303,6 +303,26 @@ def test_chunks_behind_long_contexts(kind, T, lens, page):
     c.close()
 
 
+@pytest.mark.parametrize("kind", H8.KINDS)
+@pytest.mark.parametrize("heads", [(4, 2, 64), (8, 8, 128), (6, 2, 128), (32, 8, 128), (10, 2, 64), (8, 1, 64)])
+@pytest.mark.parametrize("T,lens,page", [(2, [2, 3, 64, 65, 250], 0), (3, [1500, 3, 700], 48), (5, [129, 128, 2003, 5], 64),
+                                         (9, list(range(9, 400, 17)), 16)])
+def test_few_queries(kind, heads, T, lens, page):
+    """Queries that share a pass over their sequence, each with its own last token, with parts that begin and end inside
+    sequences; T of them, and, with the same workspace, fewer."""
+    import torch
+    c = H8.Case(kind, *heads, lens, page=page, style=T % 2, theta=500000.0, seed=T, flags=H.lib().LORC_FLAG_DEBUG_FP32)
+    c.workspace(T)
+    for t in (T, T - 1):
+        q, qd = c.queries(t, scale=2.0)
+        out = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device="cuda")
+        c.L.lorc_prefill_attn8(c.ctx, 0, c.cache(), qd, out, t)
+        assert c.L.lorc_last_path(c.ctx) == 3
+        H8.assert_attention(H.host_f64(out), *c.want(q, t))
+        assert c.status() == 0 and c.guard_intact()
+    c.close()
+
+
 @pytest.mark.parametrize("heads", [(32, 8, 128), (4, 2, 64)])
 def test_a_chunk_longer_than_a_sequence(heads):
     import torch
@@ -321,7 +341,7 @@ def test_a_chunk_longer_than_a_sequence(heads):
 def test_chunks_report_numbers_beyond_fp16(kind, which):
     """The tcgen05 path holds keys and values in fp16: up to 65504 they count, what is larger is reported."""
     import torch
-    c = H8.Case(kind, 32, 8, 128, [300, 200], seed=11)
+    c = H8.Case(kind, 32, 8, 128, [1500, 200], seed=11)
     largest = C8.LARGEST[kind]
     c.codes[which][1, 100, 5] = largest
     fits = 2.0 ** np.floor(np.log2(65504 / largest))
