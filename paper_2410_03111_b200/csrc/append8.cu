@@ -1,5 +1,6 @@
 // Cache write of uncompressed layers in 8 bits: [K | V] = x [W_k | W_v], keys rotated, both rounded to codes with one scale per
-// block of 16 tokens and KV head.  Prompt-sized launches run in append8_tc.cu; here are the others.
+// block of 16 tokens and KV head.  Here are the kernels for a handful of tokens, the plain ones, and the choice; batches of steps and
+// short prompts run in append8_split.cu, others in append8_tc.cu.
 //
 // Two kernels.  The projection leaves fp32 numbers [tokens][2 n] in the workspace; the second kernel has a block of threads for each
 // (block of tokens, KV head, keys or values), which sees all numbers that share a scale.  16 sequences, D 4096, 8 KV heads of 128
@@ -198,17 +199,39 @@ quantize8_kernel(const Append8Params p, const float* __restrict__ proj, int pair
 
 }  // namespace
 
+// Expected time of the kernels of this file in tenths of a microsecond: every tile of 16 tokens streams the factor.
+static long long mma_time(const lorc_ctx* ctx, long long tiles) {
+    return 44 + tiles * (2 * ctx->n) * (14 + 30 * ctx->desc.d_model / 4096) / 2048;
+}
+
+constexpr long long MMA_TILES = 64;      // (beyond them every way is faster)
+
+// The kernels for a call: those that should take least.  Measured, us, 8 KV heads of 128 dimensions, D 4096 (sequences x tokens), these
+// kernels / D split over clusters / prompts: 1 x 1 6.5 / 8.9 / 21, 16 x 1 8.7 / 9.2 / 21, 32 x 1 13.2 / 9.5 / 22, 64 x 1 22 / 10 / 22,
+// 256 x 1 - / 15 / 55, 512 x 1 - / 32 / 118, 64 x 4 62 / 16 / 32, 1 x 48 17 / 11 / 21, 1 x 120 - / 16 / 21, 1 x 250 - / 25 / 22,
+// 16 x 20 - / 48 / 22; D 8192: 16 x 1 11.9 / 11.7 / 36, 128 x 1 - / 16 / 52.
+Append8Way lorc_append8_way(const lorc_ctx* ctx, int batch, int T) {
+    const long long tiles = ((long long)batch * T + 15) / 16;
+    const bool split = lorc_append8_split_supported(ctx, batch, T), tc = lorc_append8_tc_supported(ctx);
+    Append8Way way = APPEND8_MMA;
+    long long least = (split || tc) && tiles > MMA_TILES ? 1ll << 62 : mma_time(ctx, tiles);
+    if (tc && lorc_append8_tc_time(ctx, batch, T) < least) {
+        way = APPEND8_TC;
+        least = lorc_append8_tc_time(ctx, batch, T);
+    }
+    if (split && lorc_append8_split_time(ctx, batch, T) < least) way = APPEND8_SPLIT;
+    return way;
+}
+
 size_t lorc_append8_scratch_bytes(const lorc_ctx* ctx, int batch, int T) {
-    if (lorc_append8_tc_supported(ctx, batch, T)) return 0;
+    if (lorc_append8_way(ctx, batch, T) != APPEND8_MMA) return 0;
     return lorc_align_up((size_t)batch * T * 2 * ctx->n * sizeof(float), 256);
 }
 
 size_t lorc_append8_scratch_most(const lorc_ctx* ctx, int batch, int T) {
-    // a call with fewer tokens may run on the other kernels
-    const long long all = (long long)batch * T;
-    long long n = all;
-    if (lorc_append8_tc_supported(ctx, batch, T))
-        for (n = 0; n + 16 <= all && !lorc_append8_tc_supported(ctx, 1, (int)n + 16);) n += 16;
+    // a call with fewer tokens may run on the kernels that need scratch
+    long long n = (long long)batch * T;
+    if (lorc_append8_tc_supported(ctx) && n > MMA_TILES * 16) n = MMA_TILES * 16;
     return lorc_align_up((size_t)n * 2 * ctx->n * sizeof(float), 256);
 }
 
@@ -221,7 +244,9 @@ cudaError_t lorc_append8_launch(lorc_ctx* ctx, const LorcLayer& L, const Cache8V
     p.cv = cv; p.rope_table = ctx->rope_table; p.status = ctx->status_dev; p.T = T; p.max_pos = ctx->desc.max_pos;
     p.n_blocks = (T + LORC_BLOCK8 - 2) / LORC_BLOCK8 + 1;
     p.interleaved = ctx->pair_style == LORC_ROPE_INTERLEAVED;
-    if (lorc_append8_tc_supported(ctx, cv.batch, T)) return lorc_append8_tc_launch(ctx, L, p, x, st, launches);
+    const Append8Way way = lorc_append8_way(ctx, cv.batch, T);
+    if (way == APPEND8_SPLIT) return lorc_append8_split_launch(ctx, L, p, x, st, launches);
+    if (way == APPEND8_TC) return lorc_append8_tc_launch(ctx, L, p, x, st, launches);
     const bool mma = D % 256 == 0 && L.A_tiled != nullptr && !(ctx->desc.flags & LORC_FLAG_DEBUG_FP32);
     // grid rows are limited to 65535: chunks of as many tokens
     const int tile = mma ? 16 : 8;

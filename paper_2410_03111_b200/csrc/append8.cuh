@@ -107,6 +107,12 @@ __device__ __forceinline__ uint4 append8_recode(const uint4& c, float keep) {
     return append8_codes<E4M3>(x, keep, false);
 }
 
+// Few tokens, D split over a cluster (append8_split.cu).
+bool lorc_append8_split_supported(const lorc_ctx* ctx, int batch, int T);
+long long lorc_append8_split_time(const lorc_ctx* ctx, int batch, int T);
+cudaError_t lorc_append8_split_launch(lorc_ctx* ctx, const LorcLayer& L, const Append8Params& q, const bf16* x, cudaStream_t st, int* launches);
+
 // Prompt-sized launches (append8_tc.cu).
-bool lorc_append8_tc_supported(const lorc_ctx* ctx, int batch, int T);
+bool lorc_append8_tc_supported(const lorc_ctx* ctx);
+long long lorc_append8_tc_time(const lorc_ctx* ctx, int batch, int T);
 cudaError_t lorc_append8_tc_launch(lorc_ctx* ctx, const LorcLayer& L, const Append8Params& q, const bf16* x, cudaStream_t st, int* launches);

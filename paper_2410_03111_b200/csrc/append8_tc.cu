@@ -333,13 +333,15 @@ append8_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constan
 
 }  // namespace
 
-// Whether a launch runs here.  The other kernels' time goes with the tiles of 16 tokens, each of which streams the factor; here a unit
-// of 256 rows takes the same time however few of them are tokens.  (8 KV heads of 128 dimensions, D 4096, us there and here: one
-// sequence's 48 tokens 17 and 21, 64 tokens 21 and 21; 64 x 1 tokens 22 and 22, 200 x 1 64 and 54, 16 x 16 61 and 22, 64 x 4 62 and 32.)
-bool lorc_append8_tc_supported(const lorc_ctx* ctx, int batch, int T) {
-    if (ctx->desc.d_model % KC || !lorc_get_tmap_encode() || (ctx->desc.flags & LORC_FLAG_DEBUG_FP32)) return false;
-    const long long n_tok = (long long)batch * T;
-    return 2 * ctx->n / 8 * ((n_tok + 15) / 16) > 6ll * ctx->sm_count;
+bool lorc_append8_tc_supported(const lorc_ctx* ctx) {
+    return ctx->desc.d_model % KC == 0 && lorc_get_tmap_encode() && !(ctx->desc.flags & LORC_FLAG_DEBUG_FP32);
+}
+
+// Expected time in tenths of a microsecond: rounds of the persistent pairs over units of 256 rows x 128 columns.
+long long lorc_append8_tc_time(const lorc_ctx* ctx, int batch, int T) {
+    const long long blocks = (long long)batch * ((T + LORC_BLOCK8 - 2) / LORC_BLOCK8 + 1), units = (blocks + 15) / 16 * (2 * ctx->n / 128);
+    const long long slots = ctx->sm_count / 2;
+    return 80 + (units + slots - 1) / slots * 125 * ctx->desc.d_model / 4096;
 }
 
 cudaError_t lorc_append8_tc_launch(lorc_ctx* ctx, const LorcLayer& L, const Append8Params& q, const bf16* x, cudaStream_t st, int* launches) {

@@ -94,6 +94,8 @@ __device__ __forceinline__ float lorc_scale8(float most) {
 // ---- host side ----------------------------------------------------------------------------------------------------------
 // Projection and quantisation (append8.cu): x [batch, T, D] -> codes.  Scratch of a call, and of any call with at most as many
 // sequences and tokens.
+enum Append8Way { APPEND8_MMA, APPEND8_SPLIT, APPEND8_TC };
+Append8Way lorc_append8_way(const lorc_ctx* ctx, int batch, int T);
 size_t lorc_append8_scratch_bytes(const lorc_ctx* ctx, int batch, int T);
 size_t lorc_append8_scratch_most(const lorc_ctx* ctx, int batch, int T);
 cudaError_t lorc_append8_launch(lorc_ctx* ctx, const LorcLayer& L, const Cache8View& cv, const bf16* x, int T, void* scratch,

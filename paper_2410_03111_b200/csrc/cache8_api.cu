@@ -118,7 +118,7 @@ int lorc_append8(lorc_ctx* ctx, int layer, const lorc_cache8* cache, const void*
     LorcStageTimer timer(ctx, LORC_STAGE_APPEND, (cudaStream_t)stream);
     const cudaError_t e = lorc_append8_launch(ctx, ctx->layers[layer], cv, (const bf16*)x, T, ctx->ws, (cudaStream_t)stream, &launches);
     ctx->launches += launches;
-    ctx->last_path = lorc_append8_tc_supported(ctx, cv.batch, T) ? 2 : ctx->desc.flags & LORC_FLAG_DEBUG_FP32 ? 1 : 3;
+    ctx->last_path = lorc_append8_way(ctx, cv.batch, T) != APPEND8_MMA ? 2 : ctx->desc.flags & LORC_FLAG_DEBUG_FP32 ? 1 : 3;
     return e == cudaSuccess ? LORC_OK : fail8_cuda(ctx, e, "lorc_append8");
 }
 

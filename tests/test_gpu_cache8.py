@@ -459,6 +459,51 @@ def test_write_of_single_tokens(kind, style, heads, D, b):
 
 
 @pytest.mark.parametrize("kind", H8.KINDS)
+@pytest.mark.parametrize("heads,D", [((8, 8, 128), 512), ((17, 17, 64), 512), ((8, 8, 128), 8192)])
+@pytest.mark.parametrize("T,lens", [(1, [1 + (29 * s) % 67 for s in range(37)]), (1, [5 + s % 40 for s in range(150)]),
+                                    (3, [3 + (7 * s) % 50 for s in range(24)]), (16, [16 + s for s in range(7)]),
+                                    (20, [20, 33, 47]), (70, [75])])
+def test_write_of_few_tokens(kind, heads, D, T, lens):
+    """Batches of decode steps, drafts and short prompts, with D split over a cluster."""
+    test_write_of_gaussian_tokens(kind, T % 2, heads, D, T, lens)
+    if D == 512:
+        test_write_is_exact_where_the_projection_is(kind, heads, D, T, lens, 16 if T == 3 else 0)
+
+
+@pytest.mark.parametrize("kind", H8.KINDS)
+@pytest.mark.parametrize("T,lens", [(1, [17 + s % 30 for s in range(40)]), (5, [20, 40, 61, 33, 44])])
+def test_finite_numbers_beside_others_in_small_batches(kind, T, lens):
+    test_finite_numbers_beside_others_count_for_the_scale(kind, T, lens, path=2)
+
+
+@pytest.mark.parametrize("kind", H8.KINDS)
+def test_small_batches_beyond_the_capacity_and_in_bad_pages(kind):
+    """Of a batch of single tokens and of pairs, only those with a place are written; all is reported."""
+    import torch
+    for T in (1, 2):
+        c = H8.Case(kind, 8, 8, 128, [20 + s for s in range(24)], page=16, D=512, seed=T, max_len=64)
+        before, sc = c.kv.clone(), c.sc.clone()
+        x = torch.ones(24, T, 512, dtype=torch.bfloat16, device="cuda")
+        c.workspace(T)
+        c.sl.copy_(torch.tensor([49] * 20 + [65, -3, 0, 40], dtype=torch.int32))
+        c.table[:, 3] = 10 ** 6
+        c.table[:, 2] = -1
+        c.table[0] = torch.arange(4, dtype=torch.int32, device="cuda") + 3
+        owned = [3 + 3] if T == 1 else [3 + 2, 3 + 3]
+        c.L.lorc_append8(c.ctx, 0, c.cache(), x, T)
+        assert c.L.lorc_last_path(c.ctx) == 2 and c.status() == c.L.LORC_ERR_CAPACITY
+        changed = (c.kv != before).any(-1)
+        rows = {(p, r) for _, p, r in changed.nonzero().tolist()}
+        # position 48 (T = 1), 47 and 48 (T = 2), of sequence 0
+        want = {(6, 0)} if T == 1 else {(5, 15), (6, 0)}
+        assert want <= rows
+        assert all(p in owned for p, _ in rows)          # (earlier tokens of the block may be under a larger scale)
+        scales = {p for _, p, b, _ in (c.sc != sc).nonzero().tolist()}
+        assert scales <= set(owned)
+        c.close()
+
+
+@pytest.mark.parametrize("kind", H8.KINDS)
 def test_numbers_that_are_not_finite(kind):
     """They are reported and contained: NaN becomes 0, an infinity the largest code, other heads and blocks are as ever."""
     import torch
@@ -481,7 +526,7 @@ def test_numbers_that_are_not_finite(kind):
 
 @pytest.mark.parametrize("kind", H8.KINDS)
 @pytest.mark.parametrize("T,lens", [(1, [17, 40]), (2, [40]), (100, [140])])
-def test_finite_numbers_beside_others_count_for_the_scale(kind, T, lens):
+def test_finite_numbers_beside_others_count_for_the_scale(kind, T, lens, path=None):
     """The largest finite numbers of a block stand next to a NaN and an infinity: codes and scales are the oracle's."""
     c = H8.Case(kind, 8, 8, 128, lens, D=512, style=H.ROPE_NONE, seed=T + 30)
     w = np.asarray(c.w[1]).copy()
@@ -511,7 +556,7 @@ def test_finite_numbers_beside_others_count_for_the_scale(kind, T, lens):
     c.workspace(T)
     c.L.lorc_append8(c.ctx, 0, c.cache(), H.dev_bf16(x), T)
     assert c.status() == c.L.LORC_ERR_ARG
-    assert c.L.lorc_last_path(c.ctx) == (2 if T == 100 else 3)
+    assert c.L.lorc_last_path(c.ctx) == (path or (2 if T == 100 else 3))
     assert np.array_equal(c.sc.double().cpu().numpy(), want_scales)
     assert np.array_equal(H8.host_codes(c.kv, kind), want_codes)
     c.close()
