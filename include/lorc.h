@@ -337,8 +337,8 @@ int lorc_decode_attn8(lorc_ctx* ctx, int layer, const lorc_cache8* cache, const 
 
 /* Attention of the T newest tokens of every sequence, as lorc_prefill_attn, over the 8-bit cache: q, out
  * [batch, T, n_q_heads, d_head] bf16; the T tokens are already cached, and query t sees the tokens up to its own.  A
- * sequence with fewer than T tokens gets zeros, and status ARG (EMPTY if it has none).  With the head geometries of the
- * tcgen05 kernels, unless there are few queries, keys and values are brought to fp16 in the workspace once per call: code x
+ * sequence with fewer than T tokens gets zeros, and status ARG (EMPTY if it has none).  Unless
+ * there are few queries (or the debug flag is set), keys and values are brought to fp16 in the workspace once per call: code x
  * scale must not exceed 65504 there (status ARG, and what comes of infinities), has steps of 2^-24 below 2^-14, and
  * tokens whose page lies outside the pool count as zeros.
  * Errors: ARG, LAYER, UNSUPPORTED (a compressed layer), WORKSPACE; CAPACITY / EMPTY / ARG through the status word. */

@@ -100,7 +100,7 @@ size_t lorc_cache8_workspace_bytes(const lorc_ctx* ctx, int batch, int max_seq_l
     size_t need = lorc_append8_scratch_most(ctx, batch, T);
     const size_t d = lorc_decode8_scratch_bytes(ctx, batch, max_seq_len, T);
     if (d > need) need = d;
-    if (T > 1 && lorc_tc_prefill_shape_ok(ctx)) {
+    if (T > 1 && !(ctx->desc.flags & LORC_FLAG_DEBUG_FP32)) {
         const size_t f = lorc_prefill8_scratch_most(ctx, batch, max_seq_len, T);
         if (f > need) need = f;
     }

@@ -89,7 +89,7 @@ struct Split8 {
 // per unit and 48 as chosen here, 512 tokens 150 and 100.  8 x 512 tokens behind 3584, 512 units on 148 SMs: 325 us in four rounds, 318
 // with the last 68 units shared by two CTAs each.)
 Split8 prefill8_split(const lorc_ctx* ctx, int batch, int max_seq_len, int T) {
-    const int qp = 256 / ctx->group;
+    const int qp = 2 * (128 / ctx->group);
     const long long P = ctx->sm_count, tiles = ((long long)max_seq_len + 127) / 128;
     Split8 best;
     best.units = best.whole = (long long)batch * ctx->desc.n_kv_heads * ((T + qp - 1) / qp);
@@ -120,9 +120,10 @@ size_t expand8_bytes(const lorc_ctx* ctx, int batch, int max_seq_len) {
 // Few queries per sequence are better served by the streaming kernel, which reads the codes once per lorc_decode8_queries of them (from
 // L2, mostly) and is then bound by its arithmetic: 0.33 us per 64 tokens, pass and KV head on an SM, against 1.3 us to expand them for
 // all queries.  (8 KV heads of 128 dimensions in groups of four, us here and there: 8 x 4096 tokens, 4 queries 31 and 87, 16 queries
-// 90 and 87, 32 queries 161 and 89; one sequence of 1000 tokens, 32 queries 15 and 20; of 8000, 32 queries 49 and 41.)
+// 90 and 87, 32 queries 161 and 89; one sequence of 1000 tokens, 32 queries 15 and 20; of 8000, 32 queries 49 and 41.  8 x 512 queries
+// of 4096 tokens, heads of 64 in groups of four, 1513 and 254; heads of 128 in groups of five 4279 and 434, ungrouped 1144 and 231.)
 bool lorc_prefill8_supported(const lorc_ctx* ctx, const Cache8View& cv, int T) {
-    if (T == 1 || cv.batch > 65535 || !lorc_tc_prefill_shape_ok(ctx) || (ctx->desc.flags & LORC_FLAG_DEBUG_FP32)) return false;
+    if (T == 1 || cv.batch > 65535 || (ctx->desc.flags & LORC_FLAG_DEBUG_FP32)) return false;
     const long long units = (long long)cv.batch * cv.n_kv * ((cv.max_seq_len + 63) / 64), P = ctx->sm_count;
     const int Q = lorc_decode8_queries(ctx, T);
     const long long stream = 80 + 33 * units * ((T + Q - 1) / Q) / (10 * P);
@@ -137,7 +138,7 @@ size_t lorc_prefill8_scratch_bytes(const lorc_ctx* ctx, int batch, int max_seq_l
 
 size_t lorc_prefill8_scratch_most(const lorc_ctx* ctx, int batch, int max_seq_len, int T) {
     // a call with fewer sequences or tokens may share more units' keys, among more CTAs: two per SM at most, and MAX_SPLIT per unit
-    const size_t qp = 256 / ctx->group, all = (size_t)batch * ctx->desc.n_kv_heads * ((T + qp - 1) / qp) * MAX_SPLIT;
+    const size_t qp = 2 * (128 / ctx->group), all = (size_t)batch * ctx->desc.n_kv_heads * ((T + qp - 1) / qp) * MAX_SPLIT;
     const size_t cap = 2 * (size_t)ctx->sm_count;
     return expand8_bytes(ctx, batch, max_seq_len) + (all < cap ? all : cap) * LORC_PREFILL_PART_FLOATS * sizeof(float);
 }

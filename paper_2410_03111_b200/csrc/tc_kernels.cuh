@@ -97,7 +97,8 @@ cudaError_t lorc_tc_prefill_set_attrs();
 cudaError_t lorc_tc_prefill_launch(lorc_ctx* ctx, const LorcLayer& L, const CacheView& cv, const CUtensorMap& mapCK,
                                    const CUtensorMap& mapCV, const CUtensorMap* mapBKT, const CUtensorMap* mapBVT,
                                    const bf16* q, bf16* out, int T, void* scratch, cudaStream_t st, int* launches);
-// Its second half: the attention over keys (rotated) and values [batch, rows, n] in fp16, rows a multiple of 128.  A
+// Its second half, for heads of 64 or 128, any number of them and both rotations: the attention over keys (rotated) and values
+// [batch, rows, n] in fp16, rows a multiple of 128.  A
 // sequence of more than max_len tokens is treated as empty (and reported).  A unit is two blocks of 128 query
 // rows of a KV head; n_split > 1: of the units behind the first `whole` ones that many CTAs share the keys, with
 // LORC_PREFILL_PART_FLOATS of scratch per unit and CTA for what they leave to a merge kernel.

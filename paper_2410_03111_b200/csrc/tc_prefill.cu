@@ -332,15 +332,16 @@ struct FaSmem {
 };
 
 struct FaParams {
-    bf16* out;                     // [b, T, H_q, 128]
+    bf16* out;                     // [b, T, H_q, DH]
     const int32_t* seq_lens;
-    const float2* rope_table;      // [max_pos][64]
+    const float2* rope_table;      // [max_pos][DH / 2]
     int* status;
     int T, H_q, G, n_rows, max_pos;
+    int interleaved;
     int nx, n_kv, unit0;           // CTAs of a sequence and KV head (a unit each, numbered in the order x, KV head, sequence); the launch's first
     int n_split;                   // SPLIT: CTAs that share the keys of a unit
     float* part_ml;                // SPLIT: [unit][n_split][256 rows][2] reference, sum of the row's probabilities
-    float* part_o;                 // SPLIT: [unit][n_split][256 rows][128] un-normalised output
+    float* part_o;                 // SPLIT: [unit][n_split][256 rows][DH] un-normalised output
 };
 
 __device__ __forceinline__ float ex2_approx(float x) {
@@ -365,12 +366,16 @@ __device__ __forceinline__ void probs_chunk(const uint32_t (&r)[32], float m, ui
     tmem_st16(taddr, w);
 }
 
+// DH: head width, 128 or 64 (then one 64-element half of everything).  GENERAL: interleaved pairs, and any G: a block has TILE / G
+// positions, and where G does not divide TILE, the rows behind them are nobody's: what stands there is multiplied along and dropped.
+// (A parameter since the code for them cost the others 2 %.)
 // SPLIT: n_split CTAs share the key tiles of the two blocks of query rows (where there are too few blocks for the SMs), in contiguous
 // equal parts; each leaves its rows' references, sums and un-normalised outputs for a merge kernel.
-template <bool SPLIT>
+template <bool SPLIT, int DH, bool GENERAL>
 __global__ void __launch_bounds__(F_THREADS, 1)
 lorc_prefill_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUtensorMap mapK,
                          const __grid_constant__ CUtensorMap mapV, const FaParams p) {
+    constexpr int HALVES = DH / 64;
     extern __shared__ uint8_t raw[];
     FaSmem& sm = *reinterpret_cast<FaSmem*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
@@ -434,11 +439,10 @@ lorc_prefill_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_
             if (elect_one()) {
                 // rows of a block: (position, head i of the KV head) -> row (position - first) * G + i; positions past the
                 // chunk read as zero
-                mbar_arrive_expect_tx(&sm.q_full, 4 * TILE * KC * 2);
-                for (int b = 0; b < 2; ++b) {
-                    tma_load_4d(sm.Q[b][0], &mapQ, &sm.q_full, 0, g * p.G, t0 + b * qp, s);
-                    tma_load_4d(sm.Q[b][1], &mapQ, &sm.q_full, 64, g * p.G, t0 + b * qp, s);
-                }
+                mbar_arrive_expect_tx(&sm.q_full, 2 * HALVES * (GENERAL ? qp * p.G : TILE) * KC * 2);
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int h = 0; h < HALVES; ++h) tma_load_4d(sm.Q[b][h], &mapQ, &sm.q_full, 64 * h, g * p.G, t0 + b * qp, s);
             }
             __syncwarp();
             for (int j = 0; j < n_tiles && ok; ++j) {
@@ -446,16 +450,18 @@ lorc_prefill_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_
                 const uint32_t par = ((j / F_STAGES) & 1) ^ 1;
                 if (!mbar_wait(&sm.k_empty[st], par)) { ok = false; break; }
                 if (elect_one()) {
-                    mbar_arrive_expect_tx(&sm.k_full[st], 2 * TILE * KC * 2);
-                    tma_load_3d(sm.K[st][0], &mapK, &sm.k_full[st], g * 128, (j_first + j) * TILE, s);
-                    tma_load_3d(sm.K[st][1], &mapK, &sm.k_full[st], g * 128 + 64, (j_first + j) * TILE, s);
+                    mbar_arrive_expect_tx(&sm.k_full[st], HALVES * TILE * KC * 2);
+#pragma unroll
+                    for (int h = 0; h < HALVES; ++h)
+                        tma_load_3d(sm.K[st][h], &mapK, &sm.k_full[st], g * DH + 64 * h, (j_first + j) * TILE, s);
                 }
                 __syncwarp();
                 if (!mbar_wait(&sm.v_empty[st], par)) { ok = false; break; }
                 if (elect_one()) {
-                    mbar_arrive_expect_tx(&sm.v_full[st], 2 * TILE * KC * 2);
-                    tma_load_3d(sm.V[st][0], &mapV, &sm.v_full[st], g * 128, (j_first + j) * TILE, s);
-                    tma_load_3d(sm.V[st][1], &mapV, &sm.v_full[st], g * 128 + 64, (j_first + j) * TILE, s);
+                    mbar_arrive_expect_tx(&sm.v_full[st], HALVES * TILE * KC * 2);
+#pragma unroll
+                    for (int h = 0; h < HALVES; ++h)
+                        tma_load_3d(sm.V[st][h], &mapV, &sm.v_full[st], g * DH + 64 * h, (j_first + j) * TILE, s);
                 }
                 __syncwarp();
             }
@@ -464,7 +470,7 @@ lorc_prefill_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_
     } else if (warp == 1) {
         if (n_tiles > 0) {
             const uint32_t idesc_s = make_idesc_f16(128, 128);            // S = Q K^T: fp16 operands, both K-major
-            const uint32_t idesc_o = make_idesc_f16(128, 128, 0, 1);      // O += P V: fp16 too, V MN-major (a key's elements are contiguous)
+            const uint32_t idesc_o = make_idesc_f16(128, DH, 0, 1);       // O += P V: fp16 too, V MN-major (a key's elements are contiguous)
             // The MMAs of one thread run in the order they were issued, and a commit covers everything issued before it:
             // when s_full[b] fires for tile j + 1, block b's P V of tile j has also finished with the probabilities that
             // these scores overwrite and with the output a softmax warp may rescale.
@@ -472,7 +478,7 @@ lorc_prefill_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_
                 const uint32_t q0 = smem_u32(sm.Q[b][0]), k0 = smem_u32(sm.K[st][0]);
                 if (elect_one()) {
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
+                    for (int k = 0; k < DH / 16; ++k) {
                         const uint32_t off = (k >> 2) * (TILE * KC * 2) + (k & 3) * 32;
                         tc_mma_bf16(tmem + b * 128, make_smem_desc_sw128(q0 + off, 0, 1024),
                                     make_smem_desc_sw128(k0 + off, 0, 1024), idesc_s, k != 0);
@@ -532,7 +538,8 @@ lorc_prefill_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_
         const int quarter = warp % 4;                            // the 32 lanes of tensor memory this warp may touch
         const int row = quarter * 32 + lane;
         const int tt = b * qp + row / p.G, hi = row % p.G;
-        const bool live = len > 0 && t0 + tt < p.T;
+        const bool mine = !GENERAL || row < qp * p.G;            // (the others are nobody's)
+        const bool live = mine && len > 0 && t0 + tt < p.T;
         const int pq = live ? len - p.T + t0 + tt : -1;          // this row's position: it sees keys 0 .. pq
         const uint32_t trow = tmem + ((uint32_t)(quarter * 32) << 16) + b * 128;   // scores / probabilities
         const uint32_t orow = tmem + ((uint32_t)(quarter * 32) << 16) + 256 + b * 128;
@@ -543,30 +550,37 @@ lorc_prefill_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_
             // at the same offset of both; elements 8 lc ... 8 lc + 7 of row r are its physical 16-byte piece lc ^ (r & 7).
             if (!mbar_wait(&sm.q_full, 0)) ok = false;
             if (ok) {
-                const float scale = rsqrtf(128.f) * LOG2E;
-                const float2* cs = p.rope_table + (long long)min(max(pq, 0), p.max_pos - 1) * 64;
+                const float scale = rsqrtf((float)DH) * LOG2E;
+                const float2* cs = p.rope_table + (long long)min(max(pq, 0), p.max_pos - 1) * (DH / 2);
                 uint4* h0 = reinterpret_cast<uint4*>(sm.Q[b][0]) + row * 8;
-                uint4* h1 = reinterpret_cast<uint4*>(sm.Q[b][1]) + row * 8;
+                uint4* h1 = HALVES == 2 ? reinterpret_cast<uint4*>(sm.Q[b][1]) + row * 8 : h0;
 #pragma unroll
-                for (int lc = 0; lc < 8; ++lc) {
+                for (int lc = 0; lc < DH / 16; ++lc) {
                     // logical piece lc of every row at once: the rows of a quarter warp then touch all eight physical
                     // pieces (no shared-memory bank conflict)
-                    const int pc = lc ^ (row & 7), j0 = 8 * lc;
-                    uint4 a = h0[pc], c = h1[pc];
+                    const int pc = lc ^ (row & 7), pd = (HALVES == 2 ? lc : lc + 4) ^ (row & 7), j0 = 8 * lc;
+                    uint4 a = h0[pc], c = h1[pd];
                     uint32_t* aw = reinterpret_cast<uint32_t*>(&a);
                     uint32_t* cw = reinterpret_cast<uint32_t*>(&c);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float4 t = __ldg(reinterpret_cast<const float4*>(cs + j0 + 2 * e));   // (cos, sin) x 2
                         const float a0 = __uint_as_float(aw[e] << 16), a1 = __uint_as_float(aw[e] & 0xffff0000u);
                         const float b0 = __uint_as_float(cw[e] << 16), b1 = __uint_as_float(cw[e] & 0xffff0000u);
-                        const __half2 x = __floats2half2_rn((a0 * t.x - b0 * t.y) * scale, (a1 * t.z - b1 * t.w) * scale);
-                        const __half2 y = __floats2half2_rn((a0 * t.y + b0 * t.x) * scale, (a1 * t.w + b1 * t.z) * scale);
+                        __half2 x, y;
+                        if (GENERAL && p.interleaved) {
+                            const float2 t = __ldg(cs + j0 / 2 + e), u = __ldg(cs + DH / 4 + j0 / 2 + e);
+                            x = __floats2half2_rn((a0 * t.x - a1 * t.y) * scale, (a0 * t.y + a1 * t.x) * scale);
+                            y = __floats2half2_rn((b0 * u.x - b1 * u.y) * scale, (b0 * u.y + b1 * u.x) * scale);
+                        } else {
+                            const float4 t = __ldg(reinterpret_cast<const float4*>(cs + j0 + 2 * e));   // (cos, sin) x 2
+                            x = __floats2half2_rn((a0 * t.x - b0 * t.y) * scale, (a1 * t.z - b1 * t.w) * scale);
+                            y = __floats2half2_rn((a0 * t.y + b0 * t.x) * scale, (a1 * t.w + b1 * t.z) * scale);
+                        }
                         aw[e] = *reinterpret_cast<const uint32_t*>(&x);
                         cw[e] = *reinterpret_cast<const uint32_t*>(&y);
                     }
                     h0[pc] = a;
-                    h1[pc] = c;
+                    h1[pd] = c;
                 }
                 fence_proxy_async_smem();      // the MMA reads the rows through the asynchronous proxy
                 __syncwarp();
@@ -614,7 +628,7 @@ lorc_prefill_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_
                 l1 *= alpha;
                 if (j > 0) {
 #pragma unroll 1
-                    for (int c0 = 0; c0 < TILE; c0 += 16) {
+                    for (int c0 = 0; c0 < DH; c0 += 16) {
                         uint32_t o[16];
                         tmem_ld16(orow + c0, o);
                         tmem_wait_ld();
@@ -645,21 +659,21 @@ lorc_prefill_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_
         }
         if (ok) {
             tc_fence_after_sync();
-            const bool has_out = t0 + tt < p.T;                // (rows past the chunk still take part in the warp-wide loads)
+            const bool has_out = mine && t0 + tt < p.T;        // (rows past the chunk still take part in the warp-wide loads)
             const float l = l0 + l1;
             if (SPLIT) {
                 const long long at = (((long long)local * p.n_split + part) * 2 + b) * TILE + row;
                 if (has_out) *reinterpret_cast<float2*>(p.part_ml + at * 2) = make_float2(m_ref, l);
                 if (n_tiles > 0) {
 #pragma unroll 1
-                    for (int c0 = 0; c0 < TILE; c0 += 16) {
+                    for (int c0 = 0; c0 < DH; c0 += 16) {
                         uint32_t o[16];
                         tmem_ld16(orow + c0, o);
                         tmem_wait_ld();
 #pragma unroll
                         for (int v = 0; v < 4; ++v)
                             if (has_out)
-                                reinterpret_cast<uint4*>(p.part_o + at * 128 + c0)[v] = make_uint4(o[4 * v], o[4 * v + 1], o[4 * v + 2], o[4 * v + 3]);
+                                reinterpret_cast<uint4*>(p.part_o + at * DH + c0)[v] = make_uint4(o[4 * v], o[4 * v + 1], o[4 * v + 2], o[4 * v + 3]);
                     }
                 }
             } else {
@@ -667,9 +681,9 @@ lorc_prefill_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_
                 // a NaN means non-finite numbers in the cache, the factors or the query (or a key beyond the fp16 range)
                 if (has_out && l != l) lorc_set_status(p.status, LORC_ERR_ARG);
                 if (has_out && !(l > 0.f) && l == l && hi == 0 && g == 0 && t0 + tt == 0) lorc_set_status(p.status, LORC_ERR_EMPTY);
-                bf16* dst = p.out + (((long long)s * p.T + (has_out ? t0 + tt : 0)) * p.H_q + g * p.G + hi) * 128;
+                bf16* dst = p.out + (((long long)s * p.T + (has_out ? t0 + tt : 0)) * p.H_q + g * p.G + hi) * DH;
     #pragma unroll
-                for (int c0 = 0; c0 < TILE; c0 += 32) {
+                for (int c0 = 0; c0 < DH; c0 += 32) {
                     uint32_t o[32];
                     if (n_tiles > 0) {
                         tmem_ld32(orow + c0, o);
@@ -699,7 +713,8 @@ lorc_prefill_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_
     if (warp == 1) tmem_dealloc(tmem, 512);
 }
 
-// Merge of the parts of a row: one warp per row, four dimensions per lane.
+// Merge of the parts of a row: one warp per row, DH / 32 dimensions per lane.
+template <int DH>
 __global__ void __launch_bounds__(256)
 lorc_prefill_merge_kernel(const FaParams p) {
     const int lane = threadIdx.x & 31, r = (int)blockIdx.x % 32 * 8 + (threadIdx.x >> 5), local = (int)blockIdx.x / 32;
@@ -707,24 +722,32 @@ lorc_prefill_merge_kernel(const FaParams p) {
     const int t = (p.nx - 1 - unit % p.nx) * 2 * qp + (r >= TILE ? qp : 0) + r % TILE / p.G, n_split = p.n_split;
     grid_dep_wait();
     grid_dep_launch();
-    if (t >= p.T) return;
+    if (t >= p.T || r % TILE >= qp * p.G) return;
+    constexpr int PER = DH / 32;
     const float* part_ml = p.part_ml + (long long)local * n_split * 2 * TILE * 2;
-    const float* part_o = p.part_o + (long long)local * n_split * 2 * TILE * 128;
+    const float* part_o = p.part_o + (long long)local * n_split * 2 * TILE * DH;
     constexpr long long rows = 2 * TILE;
     const int row = r;
     float M = -INFINITY, L = 0.f;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    float acc[PER];
+#pragma unroll
+    for (int e = 0; e < PER; ++e) acc[e] = 0.f;
     for (int c0 = 0; c0 < n_split; c0 += 4) {
         float2 ml[4];
-        float4 o[4];
+        float o[4][PER];
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
             ml[c] = make_float2(0.f, 0.f);
-            o[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int e = 0; e < PER; ++e) o[c][e] = 0.f;
             if (c0 + c < n_split) {
                 ml[c] = *reinterpret_cast<const float2*>(part_ml + ((c0 + c) * rows + row) * 2);
                 // (a part without tokens has left no output)
-                if (ml[c].y != 0.f) o[c] = *reinterpret_cast<const float4*>(part_o + ((c0 + c) * rows + row) * 128 + lane * 4);
+                const float* from = part_o + ((c0 + c) * rows + row) * DH + lane * PER;
+                if (ml[c].y != 0.f) {
+                    if (PER == 4) *reinterpret_cast<float4*>(o[c]) = *reinterpret_cast<const float4*>(from);
+                    else *reinterpret_cast<float2*>(o[c]) = *reinterpret_cast<const float2*>(from);
+                }
             }
         }
         float now = M;
@@ -734,7 +757,8 @@ lorc_prefill_merge_kernel(const FaParams p) {
         if (now > M) {
             const float alpha = M == -INFINITY ? 0.f : exp2f(M - now);
             L *= alpha;
-            acc.x *= alpha; acc.y *= alpha; acc.z *= alpha; acc.w *= alpha;
+#pragma unroll
+            for (int e = 0; e < PER; ++e) acc[e] *= alpha;
             M = now;
         }
 #pragma unroll
@@ -742,18 +766,22 @@ lorc_prefill_merge_kernel(const FaParams p) {
             if (ml[c].y == 0.f) continue;
             const float w = exp2f(ml[c].x - M);
             L += w * ml[c].y;
-            acc.x += w * o[c].x;
-            acc.y += w * o[c].y;
-            acc.z += w * o[c].z;
-            acc.w += w * o[c].w;
+#pragma unroll
+            for (int e = 0; e < PER; ++e) acc[e] += w * o[c][e];
         }
     }
     if (L != L && lane == 0) lorc_set_status(p.status, LORC_ERR_ARG);
     if (L == 0.f && lane == 0 && t == 0) lorc_set_status(p.status, LORC_ERR_EMPTY);
     const float inv = L > 0.f ? 1.f / L : 0.f;
-    const __nv_bfloat162 x = __floats2bfloat162_rn(acc.x * inv, acc.y * inv), y = __floats2bfloat162_rn(acc.z * inv, acc.w * inv);
-    *reinterpret_cast<uint2*>(p.out + (((long long)s * p.T + t) * p.H_q + g * p.G + r % p.G) * 128 + lane * 4) =
-        make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
+    uint32_t w[PER / 2];
+#pragma unroll
+    for (int e = 0; e < PER / 2; ++e) {
+        const __nv_bfloat162 x = __floats2bfloat162_rn(acc[2 * e] * inv, acc[2 * e + 1] * inv);
+        w[e] = *reinterpret_cast<const uint32_t*>(&x);
+    }
+    bf16* dst = p.out + (((long long)s * p.T + t) * p.H_q + g * p.G + r % TILE % p.G) * DH + lane * PER;
+    if (PER == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[PER / 2 - 1]);
+    else *reinterpret_cast<uint32_t*>(dst) = w[0];
 }
 
 }  // namespace
@@ -773,12 +801,15 @@ size_t lorc_tc_prefill_scratch_bytes(const lorc_ctx* ctx, int batch, int max_seq
 cudaError_t lorc_tc_prefill_set_attrs() {
     cudaError_t e = cudaFuncSetAttribute(lorc_reconstruct_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                          (int)sizeof(RecSmem) + 1024);
-    if (e == cudaSuccess)
-        e = cudaFuncSetAttribute(lorc_prefill_attn_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 (int)sizeof(FaSmem) + 1024);
-    if (e == cudaSuccess)
-        e = cudaFuncSetAttribute(lorc_prefill_attn_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 (int)sizeof(FaSmem) + 1024);
+    auto large = [&](void (*kernel)(CUtensorMap, CUtensorMap, CUtensorMap, FaParams)) {
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(FaSmem) + 1024);
+    };
+    large(lorc_prefill_attn_kernel<false, 128, false>);
+    large(lorc_prefill_attn_kernel<true, 128, false>);
+    large(lorc_prefill_attn_kernel<false, 128, true>);
+    large(lorc_prefill_attn_kernel<true, 128, true>);
+    large(lorc_prefill_attn_kernel<false, 64, true>);
+    large(lorc_prefill_attn_kernel<true, 64, true>);
     return e;
 }
 
@@ -794,11 +825,12 @@ cudaError_t lorc_tc_prefill_attend(lorc_ctx* ctx, const int32_t* seq_lens, int b
                                    const bf16* q, bf16* out, int T, long long whole, int n_split, float* parts, cudaStream_t st,
                                    int* launches) {
     const lorc_model_desc& d = ctx->desc;
+    const uint64_t dh = d.d_head;
     CUtensorMap mapQ, mapK, mapV;
     {
-        // q [b, T, H_q, 128]: box = 64 elements x G heads x 128 / G positions
-        uint64_t dims[4] = {128, (uint64_t)d.n_q_heads, (uint64_t)T, (uint64_t)batch};
-        uint64_t str[3] = {128 * 2, (uint64_t)d.n_q_heads * 128 * 2, (uint64_t)T * d.n_q_heads * 128 * 2};
+        // q [b, T, H_q, d_head]: box = 64 elements x G heads x 128 / G positions
+        uint64_t dims[4] = {dh, (uint64_t)d.n_q_heads, (uint64_t)T, (uint64_t)batch};
+        uint64_t str[3] = {dh * 2, (uint64_t)d.n_q_heads * dh * 2, (uint64_t)T * d.n_q_heads * dh * 2};
         uint32_t box[4] = {KC, (uint32_t)ctx->group, (uint32_t)(TILE / ctx->group), 1};
         if (!lorc_make_tmap_bf16(&mapQ, q, 4, dims, str, box)) return cudaErrorInvalidValue;
     }
@@ -806,24 +838,32 @@ cudaError_t lorc_tc_prefill_attend(lorc_ctx* ctx, const int32_t* seq_lens, int b
     FaParams fp;
     fp.out = out; fp.seq_lens = seq_lens; fp.rope_table = ctx->rope_table; fp.status = ctx->status_dev;
     fp.T = T; fp.H_q = d.n_q_heads; fp.G = ctx->group; fp.n_rows = max_len; fp.max_pos = d.max_pos;
-    const int qp = 2 * TILE / ctx->group;                      // query positions per CTA (two blocks of 128 rows)
+    fp.interleaved = ctx->pair_style == LORC_ROPE_INTERLEAVED;
+    const int qp = 2 * (TILE / ctx->group);                    // query positions per CTA (two blocks of 128 rows)
     fp.nx = (T + qp - 1) / qp; fp.n_kv = d.n_kv_heads; fp.unit0 = 0; fp.n_split = 1;
+    fp.part_ml = fp.part_o = nullptr;
     const long long units = (long long)fp.nx * d.n_kv_heads * batch;
     if (n_split == 1) whole = units;
     if (units * n_split > 0x7fffffffll / 32) return cudaErrorInvalidValue;
+    const bool wide = dh == 128, general = fp.interleaved || TILE % ctx->group;
     if (whole > 0) {
         *launches += 1;
-        cudaError_t e = lorc_launch_dependent(lorc_prefill_attn_kernel<false>, dim3((unsigned)whole), dim3(F_THREADS), sizeof(FaSmem) + 1024, st,
-                                              mapQ, mapK, mapV, fp);
+        cudaError_t e = lorc_launch_dependent(!wide     ? lorc_prefill_attn_kernel<false, 64, true>
+                                              : general ? lorc_prefill_attn_kernel<false, 128, true>
+                                                        : lorc_prefill_attn_kernel<false, 128, false>,
+                                              dim3((unsigned)whole), dim3(F_THREADS), sizeof(FaSmem) + 1024, st, mapQ, mapK, mapV, fp);
         if (e != cudaSuccess || whole == units) return e;
     }
     const long long rest = units - whole;
-    fp.unit0 = (int)whole; fp.n_split = n_split; fp.part_o = parts; fp.part_ml = parts + rest * n_split * 2 * TILE * 128;
+    fp.unit0 = (int)whole; fp.n_split = n_split; fp.part_o = parts; fp.part_ml = parts + rest * n_split * 2 * TILE * dh;
     *launches += 2;
-    cudaError_t e = lorc_launch_dependent(lorc_prefill_attn_kernel<true>, dim3((unsigned)(rest * n_split)), dim3(F_THREADS), sizeof(FaSmem) + 1024,
-                                          st, mapQ, mapK, mapV, fp);
+    cudaError_t e = lorc_launch_dependent(!wide     ? lorc_prefill_attn_kernel<true, 64, true>
+                                          : general ? lorc_prefill_attn_kernel<true, 128, true>
+                                                    : lorc_prefill_attn_kernel<true, 128, false>,
+                                          dim3((unsigned)(rest * n_split)), dim3(F_THREADS), sizeof(FaSmem) + 1024, st, mapQ, mapK, mapV, fp);
     if (e != cudaSuccess) return e;
-    return lorc_launch_dependent(lorc_prefill_merge_kernel, dim3((unsigned)(rest * 32)), dim3(256), 0, st, fp);
+    return lorc_launch_dependent(wide ? lorc_prefill_merge_kernel<128> : lorc_prefill_merge_kernel<64>, dim3((unsigned)(rest * 32)), dim3(256), 0,
+                                 st, fp);
 }
 
 cudaError_t lorc_tc_prefill_launch(lorc_ctx* ctx, const LorcLayer& L, const CacheView& cv, const CUtensorMap& mapCK,

@@ -124,6 +124,19 @@ class Case:
                 vmax[s, t, :, 0] = np.repeat(np.abs(v[:m]).max(axis=(0, 2)), self.G)
         return out, size, vmax
 
+    def want_some(self, q, T, some):
+        """The same for the queries `some` only."""
+        shape = (self.b, len(some), self.H_q)
+        out, size, vmax = np.zeros(shape + (self.d_h,)), np.zeros(shape + (1,)), np.zeros(shape + (1,))
+        for s, n in enumerate(self.lens):
+            k, v = self.held(0, s, n), self.held(1, s, n)
+            for i, t in enumerate(some):
+                m = n - T + t + 1
+                out[s, i], a = C8.attention(k[:m], v[:m], self.rotate(q[s, t], m - 1), self.G)
+                size[s, i, :, 0] = a
+                vmax[s, i, :, 0] = np.repeat(np.abs(v[:m]).max(axis=(0, 2)), self.G)
+        return out, size, vmax
+
     def status(self):
         return self.L.lorc_sync_status(self.ctx)
 

@@ -337,6 +337,28 @@ def test_a_chunk_longer_than_a_sequence(heads):
 
 
 @pytest.mark.parametrize("kind", H8.KINDS)
+@pytest.mark.parametrize("heads", [(4, 2, 64), (8, 8, 128), (6, 2, 128), (10, 2, 64), (7, 1, 128), (3, 3, 64), (48, 8, 64)])
+@pytest.mark.parametrize("T,lens,page,style", [(300, [300, 4000], 0, 1), (257, [300, 257, 700, 420, 2500], 64, 0), (150, [5000], 128, 2)])
+def test_prompt_chunks_of_all_heads(kind, heads, T, lens, page, style):
+    """Any number of query heads per KV head (blocks of rows that they do not fill), heads of 64, both rotations; keys shared among
+    CTAs and not."""
+    import torch
+    c = H8.Case(kind, *heads, lens, page=page, style=style, theta=500000.0, seed=T)
+    q, qd = c.queries(T, scale=1.0)
+    out = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device="cuda")
+    c.workspace(T)
+    c.L.lorc_prefill_attn8(c.ctx, 0, c.cache(), qd, out, T)
+    assert c.status() == 0 and c.guard_intact()
+    some = np.unique(np.r_[0, 1, T // 3, T - 2, T - 1, c.rng.integers(0, T, 12)])
+    got = H.host_f64(out)
+    want, size, vmax = c.want_some(q, T, some)
+    H8.assert_attention(got[:, some], want, size, vmax, fp16=True)
+    # every row has been written, from keys that it sees: rows of zeros are as unlikely as rows of sevens
+    assert not (got == 7.0).all(-1).any() and not (got == 0.0).all(-1).any()
+    c.close()
+
+
+@pytest.mark.parametrize("kind", H8.KINDS)
 @pytest.mark.parametrize("which", [0, 1])
 def test_chunks_report_numbers_beyond_fp16(kind, which):
     """The tcgen05 path holds keys and values in fp16: up to 65504 they count, what is larger is reported."""
