@@ -30,8 +30,8 @@
 //
 // Measured, 8 KV heads of 128 dimensions: 16 x 4129 tokens 30 us (4.5 TB/s), 4 x 32777 49 us (5.5), 64 sequences of 512 to
 // 16384 185 us (6.0; a copy 6.6), 128 x 300 31 us: there it is the 1.5 us per sequence and block from its last tile's
-// arrival to the next one's first products.  (Query fragments made by the queries' warp save 1 us of the 31 and cost 1.5 of the
-// 44 of 256 x 200.)
+// arrival to the next one's first products.  (Query fragments made by the queries' warp save 1 us of the 31 and cost 1 of
+// the 13 of 64 x 200.)
 #include <math.h>
 
 #include "cache8.cuh"
@@ -43,10 +43,12 @@ using namespace sm100;
 namespace {
 
 constexpr int D8_TILE = 128;         // tokens per stage (32 per consumer warp)
-constexpr int D8_UNIT = 64;          // tokens by which work is dealt out
+constexpr int D8_UNIT = 6;           // work is dealt out by 64 tokens (2^6),
+constexpr int D8_SHORT = 8;          // or, where no sequence has more than 256 (2^8), by whole sequences
 constexpr int D8_STAGES = 3;
 constexpr int D8_THREADS = 192;      // warps 0..3 consumers, warp 4 TMA and scales, warp 5 queries
 constexpr int D8_BLOCKS_PER_SM = 2;
+constexpr int D8_LIST = 128;          // rows of a list that are looked at in one go
 constexpr float D8_RAISE = 8.f, D8_SPAN = 120.f;
 constexpr float LOG2E = 1.4426950408889634f;
 
@@ -116,6 +118,7 @@ struct D8Params {
     unsigned page_magic;                        // see d8_page_of
     int rows;                                   // batch * per_seq
     int each;                                   // parts / rows, where a list has at most 128 rows
+    int unit;                                   // D8_UNIT or D8_SHORT
     int parts, least;                           // 0: a block per row and KV head; else parts of the list, of `least` steps at least
 };
 
@@ -141,7 +144,7 @@ __device__ __forceinline__ int d8_len(const D8Params& p, int r, int* status) {
     return len - max(p.T - (r - s * p.per_seq + 1) * p.Q, 0);
 }
 // Units of a row on the list; a row without tokens has one, in which its zeros are written.
-__device__ __forceinline__ int d8_weight(int len) { return len <= 0 ? 1 : (len - 1) / D8_UNIT + 1; }
+__device__ __forceinline__ int d8_weight(const D8Params& p, int len) { return len <= 0 ? 1 : ((len - 1) >> p.unit) + 1; }
 
 // What a block works on: units [f, end) of the list, beginning in row `row`, whose first unit is `first`; `per` units to a part.
 // Unit u of the list belongs to part base + u / per.  (The host sees to it that a list has fewer than 2^30 units.)
@@ -166,13 +169,13 @@ __device__ __forceinline__ D8Range d8_range(const D8Params& p, int part, int lan
     if (p.parts == 0) {
         r.row = part;
         r.f = r.first = 0;
-        r.end = r.per = d8_weight(d8_len(p, part, nullptr));
+        r.end = r.per = d8_weight(p, d8_len(p, part, nullptr));
         return r;
     }
     int w[4], sum = 0;
 #pragma unroll
-    for (int c = 0; c < 4; ++c) w[c] = c * 32 + lane < p.rows ? d8_weight(d8_len(p, c * 32 + lane, nullptr)) : 0;
-    for (int i = 128 + lane; i < p.rows; i += 32) sum += d8_weight(d8_len(p, i, nullptr));
+    for (int c = 0; c < 4; ++c) w[c] = c * 32 + lane < p.rows ? d8_weight(p, d8_len(p, c * 32 + lane, nullptr)) : 0;
+    for (int i = 128 + lane; i < p.rows; i += 32) sum += d8_weight(p, d8_len(p, i, nullptr));
     const int total = __reduce_add_sync(0xffffffffu, sum + w[0] + w[1] + w[2] + w[3]);
     r.per = max((int)((unsigned)(total + p.parts - 1) / (unsigned)p.parts), p.least);
     if (p.each > 0) {
@@ -185,7 +188,7 @@ __device__ __forceinline__ D8Range d8_range(const D8Params& p, int part, int lan
             r.first = 0;
             r.f = r.end = 0;
             if (r.row < p.rows) {
-                const int mine = d8_weight(d8_len(p, r.row, nullptr));
+                const int mine = d8_weight(p, d8_len(p, r.row, nullptr));
                 r.per = max((int)((unsigned)(mine + p.each - 1) / (unsigned)p.each), p.least);
                 r.f = (part - r.base) * r.per;
                 r.end = min(r.f + r.per, mine);
@@ -215,7 +218,7 @@ __device__ __forceinline__ D8Range d8_range(const D8Params& p, int part, int lan
 #pragma unroll
     for (int c = 0; c < 4; ++c)
         if (!found && c * 32 < p.rows) look(c * 32, w[c]);
-    for (int i0 = 128; !found && i0 < p.rows; i0 += 32) look(i0, i0 + lane < p.rows ? d8_weight(d8_len(p, i0 + lane, nullptr)) : 0);
+    for (int i0 = 128; !found && i0 < p.rows; i0 += 32) look(i0, i0 + lane < p.rows ? d8_weight(p, d8_len(p, i0 + lane, nullptr)) : 0);
     if (!found) r.end = r.f;                     // (lengths that change under way)
     return r;
 }
@@ -334,7 +337,7 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
             next.t0 += D8_TILE;
             while (next.t0 >= next.t_end) {
                 if (len > 0) {                   // this row is done
-                    const int w = d8_weight(len);
+                    const int w = d8_weight(p, len);
                     f = min(first + w, range.end);
                     first += w;
                     ++row;
@@ -349,8 +352,8 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
                     return;
                 }
                 next.s = p.T == 1 ? row : row / p.per_seq;
-                next.t0 = (f - first) * D8_UNIT;
-                next.t_end = min(len, (min(first + d8_weight(len), range.end) - first) * D8_UNIT);
+                next.t0 = (f - first) << p.unit;
+                next.t_end = min(len, (min(first + d8_weight(p, len), range.end) - first) << p.unit);
             }
             // (looked at only when the tile's turn comes: the table access is under way until then)
             const int pos = next.t0 + blk * LORC_BLOCK8;
@@ -433,7 +436,7 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
         constexpr int E = DH / 64;               // rotary pairs per lane
         int f = range.f, first = range.first;
         for (int row = range.row; f < range.end && row < p.rows && ok; ++row) {
-            const int len = d8_len(p, row, nullptr), w = d8_weight(len);
+            const int len = d8_len(p, row, nullptr), w = d8_weight(p, len);
             if (len > 0) {
                 const int nq = MULTI ? d8_queries(p, row % p.per_seq) : 1, cols = nq * G;
                 const float2* cs = p.rope_table + (long long)(len - nq) * (DH / 2) + lane * E;      // of the first query
@@ -492,10 +495,10 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
     uint32_t q_par = 0;
     int f = range.f, first = range.first;
     for (int row = range.row; f < range.end && row < p.rows; ++row) {
-        const int len = d8_len(p, row, tid == 0 ? p.status : nullptr), w = d8_weight(len);
+        const int len = d8_len(p, row, tid == 0 ? p.status : nullptr), w = d8_weight(p, len);
         const int stop = min(first + w, range.end);
         const bool whole = f == first && stop == first + w;
-        const int t_begin = (f - first) * D8_UNIT, t_end = min(len, (stop - first) * D8_UNIT);
+        const int t_begin = (f - first) << p.unit, t_end = min(len, (stop - first) << p.unit);
         const int nq = MULTI ? d8_queries(p, row % p.per_seq) : 1, cols = nq * G;
         // (of a row of several queries, heads 2 t, 2 t + 1 of the first ones see fewer tokens)
         int seen[2] = {t_end, t_end}, seen_least = t_end;
@@ -750,14 +753,18 @@ bool make_map8(CUtensorMap* map, const void* base, const Cache8View& cv, int dh,
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// How the rows of a call are dealt out.  Parts: the blocks of a KV head that are resident at once.  A block per row where rows are
-// at most four steps long, or, with several queries per sequence, where there are more rows than parts (they are about equally
-// long then, and the list would be long to search).
-void d8_plan(const lorc_ctx* ctx, int rows, int max_seq_len, int T, int* parts, int* least) {
+// How the rows of a call are dealt out.  Parts: the blocks of a KV head that are resident at once; 0: a block per row.  That spares the
+// search for a block's part, and is taken for short sequences while there are no more of them than parts (16 x 100 tokens 5.0 us, as a
+// list 6.1), and, with several queries per sequence, where the list would be long to search.  More short sequences are dealt out
+// whole, so that a block fetches the next one while it works on one (a block per row / cut by 64 tokens / whole, us: 256 x 200 tokens
+// 44 / 36.4 / 35.5, 512 x 100 66 / 50.7 / 49.9, 64 x 200 12.8 / 17.1 / 11.9).
+void d8_plan(const lorc_ctx* ctx, int rows, int max_seq_len, int T, int* parts, int* least, int* unit) {
     const int slots = D8_BLOCKS_PER_SM * ctx->sm_count / ctx->desc.n_kv_heads;      // (lorc_part_counters goes by this)
+    const bool few = max_seq_len <= 1 << D8_SHORT;
     *parts = slots > 1 ? slots : 1;
-    *least = 2;
-    if (max_seq_len <= 4 * D8_UNIT || (T > 1 && rows >= *parts)) *parts = 0;
+    *least = few ? 1 : 2;
+    *unit = few ? D8_SHORT : D8_UNIT;
+    if ((few && rows <= *parts) || (T > 1 && rows > D8_LIST && rows >= *parts)) *parts = 0;
 }
 
 size_t d8_ml_bytes(const lorc_ctx* ctx, long long slots) {
@@ -791,10 +798,11 @@ int lorc_decode8_queries(const lorc_ctx* ctx, int T) { return T < 8 / ctx->group
 
 size_t lorc_decode8_scratch_bytes(const lorc_ctx* ctx, int batch, int max_seq_len, int T) {
     // a call may have fewer queries or shorter sequences than stated here: room for the list in any case (one query: all sequences
-    // are on it; several: fewer rows than there are parts, of Q queries each)
-    int parts, least;
-    d8_plan(ctx, 1, max_seq_len > 4 * D8_UNIT ? max_seq_len : 4 * D8_UNIT + 1, 1, &parts, &least);
-    const long long Q = lorc_decode8_queries(ctx, T), one = (long long)parts + batch, several = T > 1 ? 2ll * parts * Q : 0;
+    // are on it; several: at most D8_LIST rows or as many as parts, of Q queries each)
+    int parts, least, unit;
+    d8_plan(ctx, 1, (1 << D8_SHORT) + 1, 1, &parts, &least, &unit);
+    const long long Q = lorc_decode8_queries(ctx, T), one = (long long)parts + batch;
+    const long long several = T > 1 ? (parts + (parts > D8_LIST ? parts : (long long)D8_LIST)) * Q : 0;
     const long long slots = one > several ? one : several;
     return d8_ml_bytes(ctx, slots) + lorc_align_up((size_t)slots * ctx->desc.n_q_heads * ctx->desc.d_head * sizeof(float), 256);
 }
@@ -817,7 +825,7 @@ cudaError_t lorc_decode8_launch(lorc_ctx* ctx, const Cache8View& cv, const bf16*
     p.rows = cv.batch * p.per_seq;
     const unsigned per = cv.page_table ? cv.page_size / LORC_BLOCK8 : 1;
     p.page_magic = per > 1 ? (unsigned)(((1ull << 32) + per - 1) / per) : 0;
-    d8_plan(ctx, p.rows, cv.max_seq_len, T, &p.parts, &p.least);
+    d8_plan(ctx, p.rows, cv.max_seq_len, T, &p.parts, &p.least, &p.unit);
     p.each = p.rows <= 128 ? p.parts / p.rows : 0;
     p.part_ml = (float*)scratch;
     p.part_o = (float*)((char*)scratch + d8_ml_bytes(ctx, (long long)(p.parts + p.rows) * p.Q));

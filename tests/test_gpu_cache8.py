@@ -57,6 +57,22 @@ def test_decode_long_and_ragged(kind):
         c.close()
 
 
+@pytest.mark.parametrize("kind", H8.KINDS)
+@pytest.mark.parametrize("heads,b,page", [((16, 8, 128), 90, 0), ((8, 8, 64), 170, 64), ((4, 1, 128), 400, 16)])
+def test_decode_of_many_short_sequences(kind, heads, b, page):
+    """More sequences than blocks, none longer than 256 tokens, some empty."""
+    rng = np.random.default_rng(b)
+    lens = [int(x) for x in rng.integers(1, 257, b)]
+    for s in (0, 1, 40, b - 1):
+        lens[s] = 0
+    lens[2], lens[3] = 256, 1
+    c = H8.Case(kind, *heads, lens, page=page, seed=b)
+    q, got = _decode(c)
+    H8.assert_attention(got, *c.want(q))
+    assert not got[[0, 1, 40, b - 1]].any() and c.status() == c.L.LORC_ERR_EMPTY and c.guard_intact()
+    c.close()
+
+
 def test_decode_of_many_sequences():
     """More sequences than one look at the lengths covers, with parts that begin and end inside them, and empty ones among them."""
     rng = np.random.default_rng(6)
