@@ -4,7 +4,7 @@
 //
 // Two kernels.  The projection leaves fp32 numbers [tokens][2 n] in the workspace; the second kernel has a block of threads for each
 // (block of tokens, KV head, keys or values), which sees all numbers that share a scale.  16 sequences, D 4096, 8 KV heads of 128
-// dimensions: 9.0 us, of which 2.6 are the factor's bytes at the rate of a copy; the rest is two launches in a row, and x through L2
+// dimensions: 7.8 us, of which 2.6 are the factor's bytes at the rate of a copy; the rest is two launches in a row, and x through L2
 // once per eight columns.
 #include <math.h>
 
@@ -133,10 +133,22 @@ quantize8_kernel(const Append8Params p, const float* __restrict__ proj, int pair
     const int tid = threadIdx.x, r = tid / TPR, d0 = (tid % TPR) * 16;
     const int s = (int)blockIdx.x / p.n_blocks, head = blockIdx.y;
     const bool val = blockIdx.z != 0;
+    // What does not depend on the projection is looked up while that runs (16 x 1 tokens 8.7 us, now 7.3).  Each of its blocks has waited
+    // for the kernels in front of it before it lets this kernel start, and it writes nothing but `proj`; from L2, since what this
+    // SM may hold of an earlier kernel's reads is not known to be given up before the wait.
+    Append8Row row;
+    append8_row<true>(p, s, (int)blockIdx.x % p.n_blocks, r, row);
+    float* scale_at = (val ? cv.v_scale : cv.k_scale) + (row.at < 0 ? 0 : row.at) * cv.n_kv + head;
+    const float before = row.at >= 0 && row.has_old ? __ldcg(scale_at) : 0.f;
+    const bool second = d0 >= DH / 2;
+    float2 cs[16];                               // of this thread's dimensions (interleaved: pairs, eight of them)
+    if (!val && row.fresh) {
+        const float2* at = p.rope_table + (long long)row.pos * (DH / 2) + (p.interleaved ? d0 / 2 : second ? d0 - DH / 2 : d0);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) cs[i] = i < 8 || !p.interleaved ? at[i] : make_float2(0.f, 0.f);
+    }
     grid_dep_wait();
     grid_dep_launch();
-    Append8Row row;
-    append8_row(p, s, (int)blockIdx.x % p.n_blocks, r, row);
     if (row.at < 0) return;                      // (the whole block of threads)
     float x[16];
 #pragma unroll
@@ -147,22 +159,20 @@ quantize8_kernel(const Append8Params p, const float* __restrict__ proj, int pair
 #pragma unroll
             for (int i = 0; i < 16; i += 4) *reinterpret_cast<float4*>(x + i) = *reinterpret_cast<const float4*>(src + d0 + i);
         } else {
-            const float2* cs = p.rope_table + (long long)row.pos * (DH / 2);
             if (p.interleaved) {
 #pragma unroll
                 for (int i = 0; i < 16; i += 2) {
-                    const float2 ab = *reinterpret_cast<const float2*>(src + d0 + i), c = cs[(d0 + i) / 2];
+                    const float2 ab = *reinterpret_cast<const float2*>(src + d0 + i), c = cs[i / 2];
                     x[i] = ab.x * c.x - ab.y * c.y;
                     x[i + 1] = ab.x * c.y + ab.y * c.x;
                 }
             } else {
-                const bool second = d0 >= DH / 2;
                 const int j0 = second ? d0 - DH / 2 : d0;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const int j = j0 + i;
                     const float a = src[pairs_adjacent ? 2 * j : j], b = src[pairs_adjacent ? 2 * j + 1 : j + DH / 2];
-                    const float2 c = cs[j];
+                    const float2 c = cs[i];
                     x[i] = second ? a * c.y + b * c.x : a * c.x - b * c.y;
                 }
             }
@@ -177,10 +187,7 @@ quantize8_kernel(const Append8Params p, const float* __restrict__ proj, int pair
         most_s[tid >> 5] = most;
         odd_s[tid >> 5] = any_odd;
     }
-    // (read by all threads before the barrier, written by one behind it)
-    float* scale_at = (val ? cv.v_scale : cv.k_scale) + row.at * cv.n_kv + head;
-    const float before = row.has_old ? *scale_at : 0.f;
-    __syncthreads();
+    __syncthreads();                             // (`before` has been read by all threads: one writes its place)
     int bad = 0;
 #pragma unroll
     for (int w = 0; w < WARPS; ++w) {
@@ -201,21 +208,22 @@ quantize8_kernel(const Append8Params p, const float* __restrict__ proj, int pair
 
 // Expected time of the kernels of this file in tenths of a microsecond: every tile of 16 tokens streams the factor.
 static long long mma_time(const lorc_ctx* ctx, long long tiles) {
-    return 44 + tiles * (2 * ctx->n) * (14 + 30 * ctx->desc.d_model / 4096) / 2048;
+    return 40 + tiles * (2 * ctx->n) * (15 + 28 * ctx->desc.d_model / 4096) / 2048;
 }
 
 constexpr long long MMA_TILES = 64;      // (beyond them every way is faster)
 
 // The kernels for a call: those that should take least.  Measured, us, 8 KV heads of 128 dimensions, D 4096 (sequences x tokens), these
-// kernels / D split over clusters / prompts: 1 x 1 6.5 / 8.9 / 21, 16 x 1 8.7 / 9.2 / 21, 32 x 1 13.2 / 9.5 / 22, 64 x 1 22 / 10 / 22,
+// kernels / D split over clusters / prompts: 1 x 1 5.6 / 8.9 / 21, 16 x 1 7.4 / 9.4 / 21, 32 x 1 11.5 / 9.7 / 22, 64 x 1 19 / 10.4 / 22,
 // 256 x 1 - / 15 / 55, 512 x 1 - / 32 / 118, 64 x 4 62 / 16 / 32, 1 x 48 17 / 11 / 21, 1 x 120 - / 16 / 21, 1 x 250 - / 25 / 22,
-// 16 x 20 - / 48 / 22; D 8192: 16 x 1 11.9 / 11.7 / 36, 128 x 1 - / 16 / 52.
+// 16 x 20 - / 48 / 22; D 8192: 16 x 1 10.6 / 12 / 36, 32 x 1 17.9 / 12.2 / 36, 128 x 1 56 / 17 / 52; 32 KV heads: 16 x 1 23.8 / 27.3,
+// 32 x 1 39 / 28; 8 KV heads of 64, D 2048: 16 x 1 5.6 / 6.8, 64 x 1 10.7 / 7.1.
 Append8Way lorc_append8_way(const lorc_ctx* ctx, int batch, int T) {
     const long long tiles = ((long long)batch * T + 15) / 16;
     const bool split = lorc_append8_split_supported(ctx, batch, T), tc = lorc_append8_tc_supported(ctx);
     Append8Way way = APPEND8_MMA;
     long long least = (split || tc) && tiles > MMA_TILES ? 1ll << 62 : mma_time(ctx, tiles);
-    if (tc && lorc_append8_tc_time(ctx, batch, T) < least) {
+    if (tc && tiles > 1 && lorc_append8_tc_time(ctx, batch, T) < least) {
         way = APPEND8_TC;
         least = lorc_append8_tc_time(ctx, batch, T);
     }

@@ -18,12 +18,13 @@ struct Append8Row {
 };
 
 // Row r of the i-th block that the new tokens of sequence s reach (s < 0: none); thread r = 0 reports what is wrong with it.
+template <bool FROM_L2 = false>
 __device__ __forceinline__ void append8_row(const Append8Params& p, int s, int i, int r, Append8Row& row) {
     row.at = -1;
     row.pos = 0;
     row.fresh = row.old = row.has_old = false;
     if (s < 0) return;
-    const int len = p.cv.seq_lens[s];
+    const int len = FROM_L2 ? __ldcg(p.cv.seq_lens + s) : p.cv.seq_lens[s];
     const bool fits = len >= 0 && len <= p.cv.max_seq_len && len <= p.max_pos && len <= p.cv.capacity;
     // a sequence that is too long, or shorter than what is written to it, is reported; of the latter the tokens that have a place
     // are written
@@ -31,7 +32,7 @@ __device__ __forceinline__ void append8_row(const Append8Params& p, int s, int i
     if (!fits) return;
     const int begin = max(len - p.T, 0), blk = begin / LORC_BLOCK8 + i;
     if (blk * LORC_BLOCK8 >= len) return;
-    row.at = lorc_block8(p.cv, s, blk);
+    row.at = lorc_block8<FROM_L2>(p.cv, s, blk);
     if (row.at < 0) {
         if (r == 0) lorc_set_status(p.status, LORC_ERR_CAPACITY);
         return;

@@ -366,7 +366,8 @@ bool lorc_append8_split_supported(const lorc_ctx* ctx, int batch, int T) {
 long long lorc_append8_split_time(const lorc_ctx* ctx, int batch, int T) {
     const long long groups = split_groups(batch, T), tiles = (groups + GROUPS - 1) / GROUPS, clusters = tiles * (2 * ctx->n / TILE);
     const long long slots = 2 * ctx->sm_count / (CTAS + 1), D = ctx->desc.d_model;
-    if (clusters <= slots / 2) return 60 + 25 * D / 4096 + 6 * (groups < GROUPS ? groups : GROUPS);
+    if (clusters <= slots / 4) return 52 + 24 * D / 4096 + 2 * (groups < GROUPS ? groups : GROUPS);
+    if (clusters <= slots / 2) return 62 + 24 * D / 4096 + 6 * (groups < GROUPS ? groups : GROUPS);
     return (clusters + slots - 1) / slots * (105 + 50 * D / 4096);
 }
 

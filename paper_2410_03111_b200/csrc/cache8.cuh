@@ -20,12 +20,15 @@ struct Cache8View {
 // Number of the block (of 16 rows) that holds positions 16 blk .. of sequence s, in the cache's order of blocks; -1: it lies
 // outside the capacity or its page outside the pool.  Row i of the block is row 16 * number + i of the codes, and its scales
 // start at number * n_kv.
+// FROM_L2: for a kernel that asks before it has waited for the one in front (and knows that nothing is being written there).
+template <bool FROM_L2 = false>
 __device__ __forceinline__ long long lorc_block8(const Cache8View& c, int s, int blk) {
     const long long pos = (long long)blk * LORC_BLOCK8;
     if (blk < 0 || pos >= c.capacity) return -1;
     if (c.page_table == nullptr) return (long long)s * (c.seq_stride / LORC_BLOCK8) + blk;
     const int per = c.page_size / LORC_BLOCK8, lp = blk / per;
-    const int page = c.page_table[(long long)s * c.max_pages_per_seq + lp];
+    const int32_t* at = c.page_table + (long long)s * c.max_pages_per_seq + lp;
+    const int page = FROM_L2 ? __ldcg(at) : *at;
     if (page < 0 || page >= c.n_pages) return -1;
     return (long long)page * per + (blk - lp * per);
 }
