@@ -166,6 +166,6 @@ cudaError_t lorc_prefill8_launch(lorc_ctx* ctx, const Cache8View& cv, const bf16
     *launches += 1;
     if (e != cudaSuccess) return e;
     const Split8 split = prefill8_split(ctx, cv.batch, cv.max_seq_len, T);
-    return lorc_tc_prefill_attend(ctx, cv.seq_lens, cv.batch, rows, cv.max_seq_len, p.khat, p.vbuf, q, out, T, split.whole, split.S,
+    return lorc_tc_prefill_attend(ctx, cv.seq_lens, cv.batch, rows, cv.max_seq_len, p.khat, p.vbuf, q, out, T, true, split.whole, split.S,
                                   (float*)((char*)scratch + kv), st, launches);
 }

@@ -101,11 +101,13 @@ cudaError_t lorc_tc_prefill_launch(lorc_ctx* ctx, const LorcLayer& L, const Cach
 // [batch, rows, n] in fp16, rows a multiple of 128.  A
 // sequence of more than max_len tokens is treated as empty (and reported).  A unit is two blocks of 128 query
 // rows of a KV head; n_split > 1: of the units behind the first `whole` ones that many CTAs share the keys, with
-// LORC_PREFILL_PART_FLOATS of scratch per unit and CTA for what they leave to a merge kernel.
+// LORC_PREFILL_PART_FLOATS of scratch per unit and CTA for what they leave to a merge kernel.  early: the launch in front is a kernel
+// that waits for those before it and writes keys and values only (needed for all but whole units of 128-wide half-split heads in
+// groups that divide 128).
 #define LORC_PREFILL_PART_FLOATS (256 * 130)
 cudaError_t lorc_tc_prefill_attend(lorc_ctx* ctx, const int32_t* seq_lens, int batch, size_t rows, int max_len, const void* khat,
-                                   const void* vbuf, const bf16* q, bf16* out, int T, long long whole, int n_split, float* parts,
-                                   cudaStream_t st, int* launches);
+                                   const void* vbuf, const bf16* q, bf16* out, int T, bool early, long long whole, int n_split,
+                                   float* parts, cudaStream_t st, int* launches);
 cudaError_t lorc_tc_prefill(lorc_ctx* ctx, int layer, const LorcLayer& L, const CacheView& cv, const bf16* q, bf16* out,
                             int T, void* ws, size_t ws_bytes, cudaStream_t st, int* launches);
 
