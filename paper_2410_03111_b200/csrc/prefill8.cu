@@ -83,11 +83,10 @@ struct Split8 {
     long long time;              // tenths of a microsecond
 };
 
-// A CTA takes 2.2 us per tile of 128 keys and 4 us before and after, whatever runs beside it; the merge 3 us and its traffic; two
-// launches of the kernel in a row 2 us more than one.  Either all units share their keys among S CTAs, or those that the full rounds of
-// the SMs leave over.  (Whole calls, 8 KV heads of 128 dimensions in groups of four: 128 tokens behind 8000 take 152 us with one CTA
-// per unit and 48 as chosen here, 512 tokens 150 and 100.  8 x 512 tokens behind 3584, 512 units on 148 SMs: 325 us in four rounds, 318
-// with the last 68 units shared by two CTAs each.)
+// A CTA takes 2.2 us per tile of 128 keys and 4 us before and after, whatever runs beside it; the merge 3 us and its traffic.  Either
+// all units share their keys among S CTAs, or those that the full rounds of the SMs leave over.  (Whole calls, 8 KV heads of 128
+// dimensions in groups of four: 128 tokens behind 8000 took 152 us with one CTA per unit and 48 as chosen here, 512 tokens 150 and
+// 100.  8 x 512 tokens behind 3584, 512 units on 148 SMs: 325 us in four rounds, 311 with the last 68 units shared by two CTAs each.)
 Split8 prefill8_split(const lorc_ctx* ctx, int batch, int max_seq_len, int T) {
     const int qp = 2 * (128 / ctx->group);
     const long long P = ctx->sm_count, tiles = ((long long)max_seq_len + 127) / 128;
@@ -100,7 +99,7 @@ Split8 prefill8_split(const lorc_ctx* ctx, int batch, int max_seq_len, int T) {
         if (rest == 0 || (full && whole == 0)) continue;
         for (int S = 2; S <= MAX_SPLIT && 2 * S <= tiles && rest * S <= 2 * P; ++S) {
             const long long time = whole / P * (tiles * 22 + 40) + (rest * S + P - 1) / P * ((tiles + S - 1) / S * 22 + 40) + 30 +
-                                   rest * S * LORC_PREFILL_PART_FLOATS * 8 / 500000 + (full ? 20 : 0);
+                                   rest * S * LORC_PREFILL_PART_FLOATS * 8 / 500000;
             if (time < best.time) {
                 best.whole = whole;
                 best.S = S;
