@@ -49,7 +49,8 @@ constexpr int D8_STAGES = 3;
 constexpr int D8_THREADS = 192;      // warps 0..3 consumers, warp 4 TMA and scales, warp 5 queries
 constexpr int D8_BLOCKS_PER_SM = 2;
 constexpr int D8_LIST = 128;          // rows of a list that are looked at in one go
-constexpr float D8_RAISE = 8.f, D8_SPAN = 120.f;
+constexpr float D8_RAISE = 8.f;
+constexpr float D8_BELOW = 118.f, D8_ABOVE = 125.f;    // how far the reference of the weights may lie from that of the scores
 constexpr float LOG2E = 1.4426950408889634f;
 
 __device__ __forceinline__ void ldmatrix_x4(uint32_t (&r)[4], uint32_t addr) {
@@ -625,10 +626,10 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
                         l_run[e] *= m_run[e] == -INFINITY ? 0.f : ex2_approx(m_run[e] - top[e]);
                         m_run[e] = top[e];
                     }
-                    // (2^(m - w) stays a number of fp32: w is at least m - D8_SPAN, and at most m + D8_SPAN, which only scales beyond
-                    // 2^(D8_SPAN - D8_RAISE) could exceed)
+                    // w is at least m - D8_BELOW, so that p 2^(m - w) <= 2^(D8_RAISE + D8_BELOW) stays a number of fp32, and at most
+                    // m + D8_ABOVE, so that 2^(m - w) is not flushed to zero (a weight is 2^(D8_RAISE + 128 - D8_ABOVE) at most then)
                     float now = heavy[e] > w_run[e] + D8_RAISE ? heavy[e] : w_run[e];
-                    if (m_run[e] != -INFINITY) now = fminf(fmaxf(now, m_run[e] - D8_SPAN), m_run[e] + D8_SPAN);
+                    if (m_run[e] != -INFINITY) now = fminf(fmaxf(now, m_run[e] - D8_BELOW), m_run[e] + D8_ABOVE);
                     const float alpha = w_run[e] == -INFINITY ? 0.f : ex2_approx(w_run[e] - now);
                     w_run[e] = now;
                     m_to_w[e] = m_run[e] == -INFINITY ? 0.f : ex2_approx(m_run[e] - now);
@@ -639,18 +640,18 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
                     }
                 }
             }
-            // p = 2^(x - m), and the weights p c 2^(m - w) as fp16, pairs of heads
+            // p = 2^(x - m), and the weights (p 2^(m - w)) c as fp16, pairs of heads.  (In this order: c 2^(m - w) may exceed fp32 for tokens
+            // without weight, whose p is zero.)
             const float m0 = m_run[0] == -INFINITY ? 0.f : m_run[0], m1 = m_run[1] == -INFINITY ? 0.f : m_run[1];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const float c0 = v_scale[u] * m_to_w[0], c1 = v_scale[u] * m_to_w[1];
                 uint32_t ph[2];
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     const float p0 = ex2_approx(x[u][2 * j] - m0), p1 = ex2_approx(x[u][2 * j + 1] - m1);
                     l_run[0] += p0;
                     l_run[1] += p1;
-                    ph[j] = pack_half(p0 * c0, p1 * c1);
+                    ph[j] = pack_half(p0 * m_to_w[0] * v_scale[u], p1 * m_to_w[1] * v_scale[u]);
                 }
                 const uint32_t b0 = movmatrix_trans(ph[0]), b1 = movmatrix_trans(ph[1]);
                 // O^T += V^T (c P)^T

@@ -1,0 +1,82 @@
+"""The 8-bit cache where numbers, sizes and masks are at their edges."""
+import numpy as np
+import pytest
+
+import helpers as H
+import helpers8 as H8
+
+pytestmark = pytest.mark.gpu
+
+
+def _attend(c, q, T):
+    """q [b, T, H_q, d_h] (bf16-exact) -> [b, T, H_q, d_h]; T = 1 by lorc_decode_attn8."""
+    import torch
+    qd = H.dev_bf16(q)
+    out = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device="cuda")
+    c.workspace(T)
+    if T == 1:
+        c.L.lorc_decode_attn8(c.ctx, 0, c.cache(), qd, out)
+    else:
+        c.L.lorc_prefill_attn8(c.ctx, 0, c.cache(), qd, out, T)
+    return H.host_f64(out)
+
+
+def _assert_weights(c, q, got, T, some=None, fp16=False):
+    """Every element against the formula, with a bound by the weights that the tokens have.  w_i: the softmax weights, c_i: the scales
+    of the values, M: the largest code, B = sum w_i max|v_i|, A = max_i sum |q k_i| / sqrt(d).
+      2^-8 |want|                half a step of the output
+      2^-15 (1 + A) B            scores, exponentials and sums in fp32 (as in assert_attention)
+      2^-11 B                    half a step of a weight w_i c_i as an fp16 number
+      N 2^-32 M max w_i c_i      where it is a subnormal one: half a step is 2^-25, and the heaviest weight stands at 2^7 or more
+      N 2^-126 max|v|            weights that fp32 does not hold
+    fp16 (tcgen05): queries, keys and values are rounded too, 2^-10 (1 + A) B as in assert_attention."""
+    M = {"int8": 127.0, "e4m3": 448.0}[c.kind]
+    for s, n in enumerate(c.lens):
+        page, row = c.rows_of(s, n)
+        k, v, cv = c.held(0, s, n), c.held(1, s, n), np.abs(c.scales[1][page, row // 16])
+        for t in range(T) if some is None else some:
+            m = n - T + t + 1
+            qr = c.rotate(q[s, t], m - 1)
+            for h in range(c.H_q):
+                g = h // c.G
+                x = k[:m, g] @ qr[h] / np.sqrt(c.d_h)
+                A = (np.abs(k[:m, g]) @ np.abs(qr[h])).max() / np.sqrt(c.d_h)
+                w = np.exp(x - x.max())
+                w /= w.sum()
+                want, most = w @ v[:m, g], np.abs(v[:m, g]).max(-1)
+                B = w @ most
+                bound = 2.0 ** -8 * np.abs(want) + (2.0 ** -10 * (1 + A) if fp16 else 2.0 ** -11) * B + 2.0 ** -15 * (1 + A) * B + \
+                    m * 2.0 ** -32 * M * (w * cv[:m, g]).max() + m * 2.0 ** -126 * most.max()
+                off = np.abs(got[s, t, h] - want) - bound
+                assert np.isfinite(got[s, t, h]).all() and off.max() <= 0, (s, t, h, float(off.max()), float(np.abs(want).max()))
+
+
+@pytest.mark.parametrize("kind", H8.KINDS)
+@pytest.mark.parametrize("T", [1, 2, 3, 5])
+@pytest.mark.parametrize("small", [0.0, 2.0 ** -126, 2.0 ** -100, 2.0 ** -20])
+def test_large_scales_beside_small_ones(kind, T, small):
+    """The last block of a sequence has far larger values than all others, and most of the queries do not see it (or it has no weight
+    that fp32 holds): what they do see counts in full."""
+    c = H8.Case(kind, 4, 2, 64, [17, 33, 50], style=2, seed=T)
+    M = 127.0 if kind == "int8" else 448.0
+    q = H.synth.to_bf16_exact(np.repeat(c.rng.standard_normal((c.b, 1, c.H_kv, c.d_h)), c.G, axis=2)).astype(np.float64)
+    q = np.repeat(q, T, axis=1)
+    c.scales[0] = 2.0 ** -9 if kind == "int8" else 2.0 ** -11
+    for large in (8, 9, 28, 30, 60, 80):
+        for low in (False, True):
+            for s, n in enumerate(c.lens):
+                last = (n - 1) // 16
+                c.scales[1][s] = small
+                c.scales[1][s, last] = 2.0 ** large
+                for h in range(c.H_kv):
+                    x = q[s, 0, h * c.G]
+                    unit = np.clip(np.rint(-x / np.abs(x).max() * 31), -31, 31)
+                    unit = np.where(np.abs(unit) > 16, 2 * np.rint(unit / 2), unit)         # (numbers of both types)
+                    # a score of -200: no weight in fp32, and less than 2^-126 of the smallest values' share
+                    c.codes[0][s, 16 * last:, h * c.d_h:(h + 1) * c.d_h] = unit if low else unit * 0
+                    c.scales[0][s, last, h] = np.float32(200.0 * np.sqrt(c.d_h) / -(unit @ x))
+            assert np.abs(c.codes).max() <= M
+            c.upload()
+            _assert_weights(c, q, _attend(c, q, T), T)
+            c.status()
+    c.close()
