@@ -10,9 +10,12 @@
 //                                               (22 bits); the scale of the keys, 1 / sqrt(d) and log2 e multiply the fp32 sums
 //   l += 2^(S - m)
 //   O^T[d x 8]     += V^T[d x 16 tok] . Y^T     Y = c 2^(S - w) in one fp16 part, c the scale of the values: each weight is
-//                                               off by 2^-11 at most, which averages out over tokens; bf16 outputs lose 2^-8
+//                                               off by 2^-11 of itself at most, which averages out over tokens; bf16 outputs
+//                                               lose 2^-8
 //
-// m and w are raised when they are exceeded by more than 2^8.
+// m is raised to the largest score when that exceeds it by more than 2^8; w stands 2^7 below the heaviest weight, until one is 2^15
+// above it.  fp16 holds 2^15, and the room above 1 is room below: a weight below 2^-21 of the heaviest is off by 2^-32 of that one (with the
+// heaviest weight at 1, 2^-25, and tokens of less than that counted in l only).
 //
 // A 16-bit word of a row is two dimensions.  Key fragments take the dimensions in the order in which ldmatrix delivers bytes, and the
 // query fragments take the same order; for the values a transposed 8 x 8 matrix of words holds two dimensions of two tokens per
@@ -49,7 +52,8 @@ constexpr int D8_STAGES = 3;
 constexpr int D8_THREADS = 192;      // warps 0..3 consumers, warp 4 TMA and scales, warp 5 queries
 constexpr int D8_BLOCKS_PER_SM = 2;
 constexpr int D8_LIST = 128;          // rows of a list that are looked at in one go
-constexpr float D8_RAISE = 8.f;
+constexpr float D8_RAISE = 8.f;      // a reference is raised only when it is exceeded by more than this (log2 units)
+constexpr float D8_HEAD = 7.f;       // and the heaviest weight then stands at 2^7, so weights reach 2^15 as fp16 numbers
 constexpr float D8_BELOW = 118.f, D8_ABOVE = 125.f;    // how far the reference of the weights may lie from that of the scores
 constexpr float LOG2E = 1.4426950408889634f;
 
@@ -603,7 +607,7 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
             }
             // Running softmax over this warp's tokens.  The sum of p and the weighted values have references of their own (m, w): a
             // token's weight is p times its values' scale, so tokens with small values count in full also beside tokens of little
-            // weight with far larger values.  A reference is raised when it is exceeded by more than 2^8, which after the
+            // weight with far larger values.  A reference is raised when it is exceeded by more than 2^8 (2^15), which after the
             // first steps is rare, so the maximum over the warp is looked for only then.
             const float lv[2] = {d8_log2(v_scale[0]), d8_log2(v_scale[1])};
             float top[2], heavy[2];              // the largest score, and the largest weight (score + log2 of the scale), heads 2 t, 2 t + 1
@@ -613,8 +617,8 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
                 top[e] = fmaxf(a, b);
                 heavy[e] = fmaxf(a + lv[0], b + lv[1]);
             }
-            if (__any_sync(0xffffffffu, top[0] > m_run[0] + D8_RAISE || top[1] > m_run[1] + D8_RAISE || heavy[0] > w_run[0] + D8_RAISE ||
-                                            heavy[1] > w_run[1] + D8_RAISE)) {
+            if (__any_sync(0xffffffffu, top[0] > m_run[0] + D8_RAISE || top[1] > m_run[1] + D8_RAISE || heavy[0] > w_run[0] + D8_HEAD + D8_RAISE ||
+                                            heavy[1] > w_run[1] + D8_HEAD + D8_RAISE)) {
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
 #pragma unroll
@@ -628,7 +632,7 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
                     }
                     // w is at least m - D8_BELOW, so that p 2^(m - w) <= 2^(D8_RAISE + D8_BELOW) stays a number of fp32, and at most
                     // m + D8_ABOVE, so that 2^(m - w) is not flushed to zero (a weight is 2^(D8_RAISE + 128 - D8_ABOVE) at most then)
-                    float now = heavy[e] > w_run[e] + D8_RAISE ? heavy[e] : w_run[e];
+                    float now = heavy[e] > w_run[e] + D8_HEAD + D8_RAISE ? heavy[e] - D8_HEAD : w_run[e];
                     if (m_run[e] != -INFINITY) now = fminf(fmaxf(now, m_run[e] - D8_BELOW), m_run[e] + D8_ABOVE);
                     const float alpha = w_run[e] == -INFINITY ? 0.f : ex2_approx(w_run[e] - now);
                     w_run[e] = now;

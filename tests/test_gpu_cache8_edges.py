@@ -80,3 +80,29 @@ def test_large_scales_beside_small_ones(kind, T, small):
             _assert_weights(c, q, _attend(c, q, T), T)
             c.status()
     c.close()
+
+
+def _sinks(c, every):
+    """One token in `every` takes nearly all of the weight and has no value, the others stand 26 powers of two below it with values
+    of one sign.  -> the first element of a query"""
+    top, rest = 100.0 if c.kind == "int8" else 96.0, 2.0 ** -5
+    c.codes[0][:] = 0.0
+    c.codes[0][:, ::every, ::c.d_h] = top
+    c.scales[0][:] = rest
+    c.codes[1] = np.abs(c.codes[1])
+    c.codes[1][:, ::every] = 0.0
+    c.scales[1][:] = 2.0 ** -4
+    c.upload()
+    return float(H.synth.to_bf16_exact(np.array([18.2 * np.sqrt(c.d_h) / (top * rest)]))[0])
+
+
+@pytest.mark.parametrize("kind", H8.KINDS)
+@pytest.mark.parametrize("T,heads,lens", [(1, (2, 1, 64), [5000]), (3, (2, 1, 64), [5000]), (1, (8, 1, 128), [100, 20000, 1])])
+def test_many_tokens_far_below_the_heaviest(kind, T, heads, lens):
+    """(A heavy token for every warp of every block: each has a reference of its own.)"""
+    c = H8.Case(kind, *heads, lens, style=2, seed=50)
+    q = np.zeros((c.b, T, c.H_q, c.d_h))
+    q[..., 0] = _sinks(c, 32)
+    _assert_weights(c, q, _attend(c, q, T), T)
+    assert c.L.lorc_last_path(c.ctx) == 3 and c.status() == 0
+    c.close()
