@@ -321,6 +321,8 @@ lorc_reconstruct_kernel(const __grid_constant__ CUtensorMap mapCK, const __grid_
 constexpr int F_THREADS = 320;       // warp 0 TMA, warp 1 MMA, warps 2..5 softmax of block 0, warps 6..9 of block 1
 constexpr int F_STAGES = 2;
 constexpr float F_RAISE = 8.f;       // a row's reference is raised only when a tile exceeds it by more than this (log2 units)
+constexpr float F_HEAD = 7.f;        // the reference's probability is 2^7, so they reach 2^15 as fp16 numbers, and one below 2^-21 of
+                                     // the largest is off by 2^-32 of that (with 1 for the reference's 2^-25, and smaller ones lost)
 
 struct FaSmem {
     bf16 Q[2][2][TILE * KC];              // [block][64-element half][128 rows]
@@ -652,8 +654,9 @@ lorc_prefill_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_
                 }
                 if (raise) m_ref = mt;
             }
-            // probabilities (at most 2^8), rounded to fp16, packed two per column over the scores they came from
-            const float m_use = m_ref == -INFINITY ? 0.f : m_ref;     // a row that has seen nothing yet: 2^(-inf) = 0
+            // probabilities (times 2^F_HEAD, as their sum: at most 2^15), rounded to fp16, packed two per column over the scores
+            // they came from
+            const float m_use = m_ref == -INFINITY ? 0.f : m_ref - F_HEAD;     // a row that has seen nothing yet: 2^(-inf) = 0
             probs_chunk(r0, m_use, trow, l0, l1);
             probs_chunk(r1, m_use, trow + 16, l0, l1);
             tmem_wait_st();

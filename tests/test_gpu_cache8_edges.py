@@ -106,3 +106,50 @@ def test_many_tokens_far_below_the_heaviest(kind, T, heads, lens):
     _assert_weights(c, q, _attend(c, q, T), T)
     assert c.L.lorc_last_path(c.ctx) == 3 and c.status() == 0
     c.close()
+
+
+@pytest.mark.parametrize("heads", [(4, 1, 128), (6, 2, 64)])
+@pytest.mark.parametrize("T,N", [(400, 20000), (2500, 2500)])
+def test_chunks_far_below_the_heaviest(heads, T, N):
+    """(A heavy token in every tile of keys: blocks may share them.)"""
+    c = H8.Case("int8", *heads, [N], style=2, seed=51)
+    q = np.zeros((1, T, c.H_q, c.d_h))
+    q[..., 0] = _sinks(c, 128)
+    got = _attend(c, q, T)
+    assert c.L.lorc_last_path(c.ctx) == 2 and c.status() == 0
+    _assert_weights(c, q, got, T, some=(40, T // 2, T - 1), fp16=True)
+    c.close()
+
+
+def test_chunks_of_the_latent_cache_far_below_the_heaviest():
+    """The same kernel over reconstructed keys and values: factors of rank 128 that are the identity."""
+    import torch
+    L = H.lib()
+    N, T, d = 20000, 200, 128
+    ctx = L.lorc_create(1, 256, 32, 8, d, 10000.0, rope_style=H.ROPE_NONE, max_pos=N)
+    eye = torch.eye(d, dtype=torch.bfloat16, device="cuda").repeat(1, 8).contiguous()
+    a = torch.zeros(256, d, dtype=torch.bfloat16, device="cuda")
+    L.lorc_load_factors(ctx, 0, L.LORC_MODE_LATENT, d, d, a, eye, a, eye)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    k, v = torch.zeros(1, N, d, device="cuda"), torch.rand(1, N, d, generator=g, device="cuda")
+    k[0, ::128, 0], v[0, ::128] = 3.125, 0.0
+    k, v = k.bfloat16(), v.bfloat16()
+    sl = torch.tensor([N], dtype=torch.int32, device="cuda")
+    cache = L.make_cache(k, v, sl, 1, N, seq_stride=N)
+    ws = torch.zeros(L.lorc_prefill_workspace_bytes(ctx, 1, N, T), dtype=torch.uint8, device="cuda")
+    L.lorc_set_workspace(ctx, ws)
+    q = torch.zeros(1, T, 32, d, dtype=torch.bfloat16, device="cuda")
+    q[..., 0] = 18.2 * np.sqrt(d) / 3.125
+    out = torch.zeros_like(q)
+    L.lorc_prefill_attn(ctx, 0, cache, q, out, T)
+    assert L.lorc_sync_status(ctx) == 0 and L.lorc_last_path(ctx) == 2
+    x = (float(q[0, 0, 0, 0]) * k[0, :, 0].double()) / np.sqrt(d)
+    for t in (0, 77, T - 1):
+        m = N - T + t + 1
+        w = torch.softmax(x[:m], 0)
+        want = (w @ v[0, :m].double()).cpu().numpy()
+        # (as _assert_weights, fp16: A = 18.2, the values do not exceed 1)
+        B = float(w @ v[0, :m].double().abs().amax(-1))
+        bound = 2.0 ** -8 * want + (2.0 ** -10 + 2.0 ** -15) * 19.2 * B + m * 2.0 ** -32 * float(w.max())
+        assert (np.abs(H.host_f64(out[0, t]) - want) <= bound).all(), t
+    L.lorc_destroy(ctx)
