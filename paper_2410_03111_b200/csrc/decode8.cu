@@ -529,8 +529,8 @@ decode8_mma_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
             }
             most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
             most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
-            // its power of two, between 2^-100 and 2^100
-            const uint32_t e = min(max(__float_as_uint(most) >> 23, 27u), 227u);
+            // its power of two, between 2^-100 and 2^126 (the inverse is an ordinary number too; what is divided lies below 4)
+            const uint32_t e = min(max(__float_as_uint(most) >> 23, 27u), 253u);
             const float up = __uint_as_float(e << 23), down = __uint_as_float((254u - e) << 23);
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {

@@ -82,6 +82,21 @@ def test_large_scales_beside_small_ones(kind, T, small):
     c.close()
 
 
+@pytest.mark.parametrize("kind", H8.KINDS)
+@pytest.mark.parametrize("T", [1, 3])
+def test_queries_of_any_size(kind, T):
+    """Queries of 2^120 on keys of 2^-120: the scores are ordinary ones."""
+    c = H8.Case(kind, 4, 2, 64, [50, 300], style=0, seed=T + 40)
+    q = H.synth.to_bf16_exact(c.rng.standard_normal((c.b, T, c.H_q, c.d_h))).astype(np.float64)
+    for up in (90, 100, 116, 120):
+        c.scales[0] = 2.0 ** (-up - 6)
+        c.upload()
+        big = np.ldexp(q, up)
+        _assert_weights(c, big, _attend(c, big, T), T)
+        assert c.status() == 0
+    c.close()
+
+
 def _sinks(c, every):
     """One token in `every` takes nearly all of the weight and has no value, the others stand 26 powers of two below it with values
     of one sign.  -> the first element of a query"""
