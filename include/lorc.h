@@ -322,7 +322,7 @@ size_t lorc_cache8_workspace_bytes(const lorc_ctx* ctx, int batch, int max_seq_l
 /* Cache write: RoPE(x W_k) and x W_v of T new tokens per sequence, x and positions as in lorc_append, in fp32 until they
  * are rounded to codes (to nearest, ties to even).  The scale of a block and head becomes the smallest power of two 2^e,
  * -100 <= e <= 100, with which no new number exceeds the largest code (127, or 448), or stays what it is if the block holds
- * earlier tokens of the sequence under a larger one.  Where it grows, the codes of these are re-expressed under the new
+ * earlier tokens of the sequence under one that is larger in magnitude.  Where it grows, the codes of these are re-expressed under the new
  * scale (e4m3: exactly, down to its subnormal numbers; int8: one more rounding, half a step at most, and none unless the
  * scale doubles).  A NaN is stored as 0 and an infinity as the largest code; neither counts for the scale, and the status
  * becomes ARG.

@@ -201,7 +201,7 @@ quantize8_kernel(const Append8Params p, const float* __restrict__ proj, int pair
     }
     uint4* dst = reinterpret_cast<uint4*>((val ? cv.v : cv.k) + (row.at * LORC_BLOCK8 + r) * cv.n + head * DH + d0);
     if (row.fresh) *dst = append8_codes<E4M3>(x, 1.f / scale, false);
-    else if (row.old && scale != before) *dst = append8_recode<E4M3>(*dst, (before > 0.f ? before : 0.f) / scale);
+    else if (row.old && scale != before) *dst = append8_recode<E4M3>(*dst, append8_keep(before, scale));
 }
 
 }  // namespace

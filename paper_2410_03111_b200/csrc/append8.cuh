@@ -43,10 +43,16 @@ __device__ __forceinline__ void append8_row(const Append8Params& p, int s, int i
     row.has_old = begin > blk * LORC_BLOCK8;
 }
 
-// The scale of a block and head from the largest magnitude of its new numbers, and where it lies.
+// The scale of a block and head from the largest magnitude of its new numbers and the scale that its earlier tokens stand under, which
+// may be any finite number: the larger one in magnitude.
 template <bool E4M3>
 __device__ __forceinline__ float append8_scale(float most, float before) {
-    return fmaxf(lorc_scale8<E4M3>(most), before > 0.f ? before : 0.f);
+    const float scale = lorc_scale8<E4M3>(most), m = fabsf(before);
+    return m > scale && m <= 3.4028234663852886e38f ? before : scale;
+}
+// What the codes of the earlier tokens are multiplied by.
+__device__ __forceinline__ float append8_keep(float before, float scale) {
+    return fabsf(before) <= 3.4028234663852886e38f ? before / scale : 0.f;
 }
 
 // Magnitudes of finite numbers for the block's maximum; odd: one of them is not finite.

@@ -337,7 +337,7 @@ append8_split_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_cons
         if (odd) lorc_set_status(p.q.status, LORC_ERR_ARG);
     }
     if (!row.has_old || scale == before) return;
-    const float keep = (before > 0.f ? before : 0.f) / scale;
+    const float keep = append8_keep(before, scale);
     for (int r = c; r < in_block; r += LANES)
 #pragma unroll 1
         for (int j = 0; j < DH; j += 16) {

@@ -315,7 +315,7 @@ append8_tc_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constan
                     *at[0] = append8_codes<E4M3>(a[k], inv, clean);
                     *at[1] = append8_codes<E4M3>(b[k], inv, clean);
                 } else if (row.old && scale != before[k]) {
-                    const float keep = (before[k] > 0.f ? before[k] : 0.f) / scale;
+                    const float keep = append8_keep(before[k], scale);
 #pragma unroll 1
                     for (int i = 0; i < 2; ++i) *at[i] = append8_recode<E4M3>(*at[i], keep);
                 }

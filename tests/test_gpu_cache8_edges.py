@@ -168,3 +168,40 @@ def test_chunks_of_the_latent_cache_far_below_the_heaviest():
         bound = 2.0 ** -8 * want + (2.0 ** -10 + 2.0 ** -15) * 19.2 * B + m * 2.0 ** -32 * float(w.max())
         assert (np.abs(H.host_f64(out[0, t]) - want) <= bound).all(), t
     L.lorc_destroy(ctx)
+
+
+@pytest.mark.parametrize("kind", H8.KINDS)
+@pytest.mark.parametrize("b,T,D,path", [(2, 1, 256, 3), (40, 1, 512, 2), (9, 5, 512, 2), (2, 100, 512, 2), (1, 3, 200, 3)])
+def test_a_write_beside_tokens_under_any_scale(kind, b, T, D, path):
+    """Earlier tokens of a block may stand under a scale of either sign: the larger one in magnitude stays, and the numbers that they
+    stand for stay what they are."""
+    import torch
+    from oracle import cache8_oracle as C8
+    lens = [T + 1 + (29 * s) % 67 for s in range(b)]
+    c = H8.Case(kind, 8, 8, 128, lens, D=D, style=H.ROPE_NONE, seed=T + b)
+    c.scales *= np.where(c.rng.random(c.scales.shape) < 0.5, -1.0, 1.0) * np.ldexp(1.0, c.rng.integers(-4, 5, c.scales.shape))
+    c.upload()
+    at = c.rng.integers(0, D, (b, T))
+    x = np.zeros((b, T, D))
+    x[np.arange(b)[:, None], np.arange(T), at] = 1.0
+    want_codes, want_scales = c.codes.copy(), c.scales.copy()
+    for s, n in enumerate(c.lens):
+        for i in range(2):
+            new = np.asarray(c.w[i], dtype=np.float64)[at[s]].reshape(T, c.H_kv, c.d_h)
+            codes, scales = want_codes[i][s].reshape(-1, c.H_kv, c.d_h), want_scales[i][s]
+            for b0 in range((n - T) // 16 * 16, n, 16):
+                start, end = max(b0, n - T), min(b0 + 16, n)
+                fresh = new[start - (n - T):end - (n - T)]
+                scale, before = C8.scale_for(np.abs(fresh).max(axis=(0, 2)), kind), scales[b0 // 16]
+                if start > b0:
+                    scale = np.where(np.abs(before) > scale, before, scale)
+                    codes[b0:start] = C8.round_code(codes[b0:start] * (before / scale)[None, :, None], kind)
+                codes[start:end] = C8.round_code(fresh / scale[None, :, None], kind)
+                scales[b0 // 16] = scale
+    c.workspace(T)
+    c.L.lorc_append8(c.ctx, 0, c.cache(), H.dev_bf16(x), T)
+    assert c.L.lorc_last_path(c.ctx) == path
+    assert np.array_equal(c.sc.double().cpu().numpy(), want_scales)
+    assert np.array_equal(H8.host_codes(c.kv, kind), want_codes)
+    assert c.status() == 0
+    c.close()
