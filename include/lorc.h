@@ -289,6 +289,7 @@ int lorc_decode_step_host(lorc_ctx* ctx, int layer, const lorc_cache* cache, con
  * multiples of 16, so that a block lies within one page.  seq_lens, max_seq_len and the page table are as in lorc_cache.
  * Attention takes any finite scales; lorc_append8 writes powers of two.  Rows behind a sequence's end, and scales of
  * blocks wholly behind it, are neither read into a result nor written.
+ * A call has fewer than 2^30 new tokens (batch * T) and, in lorc_decode_attn8, batch * ceil(max_seq_len / 64) below 2^30.
  * A sequence longer than max_seq_len, the capacity or max_pos counts as empty (status CAPACITY); tokens whose page lies
  * outside the pool are left out (CAPACITY too).
  * With LORC_FLAG_DEBUG_FP32 the projection runs on the plain kernel and attention keeps off the tcgen05 kernels (it has no

@@ -107,6 +107,7 @@ cudaError_t lorc_append8_launch(lorc_ctx* ctx, const LorcLayer& L, const Cache8V
 // Attention of T >= 1 queries per sequence on mma.sync (decode8.cu): query t of a sequence is the decode query of the sequence cut
 // after that token, and lorc_decode8_queries of them share a pass over the sequence.
 int lorc_decode8_queries(const lorc_ctx* ctx, int T);
+bool lorc_decode8_fits(const lorc_ctx* ctx, const Cache8View& cv, int T);      // the list of its work has fewer than 2^30 units
 size_t lorc_decode8_scratch_bytes(const lorc_ctx* ctx, int batch, int max_seq_len, int T);
 cudaError_t lorc_decode8_launch(lorc_ctx* ctx, const Cache8View& cv, const bf16* q, bf16* out, int T, void* scratch,
                                 cudaStream_t st, int* launches);

@@ -43,7 +43,6 @@ int check8(lorc_ctx* ctx, int layer, const lorc_cache8* c, int T, const void* in
     if (c->max_seq_len > capacity) return fail8(ctx, LORC_ERR_ARG, "cache8: max_seq_len exceeds the cache capacity");
     if (T <= 0 || T > c->max_seq_len) return fail8(ctx, LORC_ERR_ARG, "cache8: T must be positive and not exceed max_seq_len");
     if ((long long)c->batch * T > 0x3fffffffll) return fail8(ctx, LORC_ERR_ARG, "cache8: batch * T is too large");
-    if ((long long)c->batch * T * ((c->max_seq_len - 1) / 64 + 1) >= 1ll << 30) return fail8(ctx, LORC_ERR_ARG, "cache8: batch * T * max_seq_len is too large");
     int dev = -1;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return fail8_cuda(ctx, e, "cache8");
@@ -73,6 +72,7 @@ int attend8(lorc_ctx* ctx, int layer, const lorc_cache8* cache, const void* q, v
     const int rc = check8(ctx, layer, cache, T, q, out, &cv);
     if (rc) return rc;
     const bool expand = lorc_prefill8_supported(ctx, cv, T);
+    if (!expand && !lorc_decode8_fits(ctx, cv, T)) return fail8(ctx, LORC_ERR_ARG, "cache8: batch * max_seq_len is too large (2^30 units of 64 tokens)");
     if (!lorc_get_tmap_encode()) return fail8(ctx, LORC_ERR_CUDA, "cache8: the driver offers no tensor maps");
     const size_t need = expand ? lorc_prefill8_scratch_bytes(ctx, cv.batch, cv.max_seq_len, T)
                                : lorc_decode8_scratch_bytes(ctx, cv.batch, cv.max_seq_len, T);

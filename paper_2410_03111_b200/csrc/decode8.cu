@@ -801,6 +801,15 @@ cudaError_t d8_launch(lorc_ctx* ctx, const CUtensorMap& mapK, const CUtensorMap&
 
 int lorc_decode8_queries(const lorc_ctx* ctx, int T) { return T < 8 / ctx->group ? T : 8 / ctx->group; }
 
+bool lorc_decode8_fits(const lorc_ctx* ctx, const Cache8View& cv, int T) {
+    const int Q = lorc_decode8_queries(ctx, T);
+    const long long rows = (long long)cv.batch * ((T + Q - 1) / Q);
+    int parts, least, unit;
+    d8_plan(ctx, (int)rows, cv.max_seq_len, T, &parts, &least, &unit);
+    if (parts == 0) return rows * ctx->desc.n_kv_heads <= 0x7fffffffll;            // a block per row and KV head
+    return rows * (((cv.max_seq_len - 1) >> unit) + 1) < 1ll << 30;
+}
+
 size_t lorc_decode8_scratch_bytes(const lorc_ctx* ctx, int batch, int max_seq_len, int T) {
     // a call may have fewer queries or shorter sequences than stated here: room for the list in any case (one query: all sequences
     // are on it; several: at most D8_LIST rows or as many as parts, of Q queries each)

@@ -205,3 +205,65 @@ def test_a_write_beside_tokens_under_any_scale(kind, b, T, D, path):
     assert np.array_equal(H8.host_codes(c.kv, kind), want_codes)
     assert c.status() == 0
     c.close()
+
+
+def test_many_new_tokens_under_a_long_cache():
+    """64 sequences, 8192 new tokens each, in a cache that may hold 131072 of each: write and attention are those of a shorter bound."""
+    import torch
+    L = H.lib()
+    b, T, D, d, room, most = 64, 8192, 64, 64, 131072, 8704
+    g = torch.Generator(device="cuda").manual_seed(1)
+    ctx = L.lorc_create(1, D, 1, 1, d, 10000.0, rope_style=0, max_pos=room)
+    w = torch.randn(2, D, d, generator=g, device="cuda").mul_(D ** -0.5).bfloat16()
+    L.lorc_load_factors(ctx, 0, L.LORC_MODE_FULL, 0, 0, w[0], None, w[1], None)
+    lens = T + torch.randint(0, most - T, (b,), generator=g, device="cuda", dtype=torch.int32)
+    x = torch.randn(b, T, D, generator=g, device="cuda").bfloat16()
+    q = torch.randn(b, T, 1, d, generator=g, device="cuda").bfloat16()
+    held = []
+    for bound in (most, room):
+        kv = torch.zeros(2, b, room, d, dtype=torch.int8, device="cuda")
+        sc = torch.full((2, b, room // 16, 1), 2.0 ** -100, device="cuda")
+        cache = L.make_cache8(kv[0], kv[1], sc[0], sc[1], lens, b, bound, L.LORC_CACHE8_INT8, seq_stride=room)
+        need = L.lorc_cache8_workspace_bytes(ctx, b, bound, T)
+        ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+        L.lorc_set_workspace(ctx, ws)
+        L.lorc_append8(ctx, 0, cache, x, T)
+        out = torch.zeros_like(q)
+        L.lorc_prefill_attn8(ctx, 0, cache, q, out, T)
+        assert L.lorc_sync_status(ctx) == 0
+        held.append((kv, sc, out))
+    assert torch.equal(held[0][0], held[1][0]) and torch.equal(held[0][1], held[1][1])
+    # the same averages of probabilities that were rounded to fp16 (2 2^-11 max|v| each way), rounded once each
+    kv, sc, out = held[1]
+    most = 127 * float(sc.max())
+    assert bool(((out.float() - held[0][2].float()).abs() <= 2.0 ** -7 * out.float().abs() + 2.0 ** -9 * most).all())
+    inv = 10000.0 ** (-torch.arange(0, d, 2, device="cuda", dtype=torch.float64) / d)
+    for s, t in ((0, 0), (17, 4000), (63, T - 1)):
+        m = int(lens[s]) - T + t + 1
+        k, v = [kv[i, s, :m].double() * sc[i, s].double().repeat_interleave(16, 0)[:m] for i in range(2)]
+        cs, sn = torch.cos((m - 1) * inv), torch.sin((m - 1) * inv)
+        a, z = q[s, t, 0].double().chunk(2)
+        qr = torch.cat([a * cs - z * sn, a * sn + z * cs])
+        want, size = torch.softmax(k @ qr / d ** 0.5, 0) @ v, float((k.abs() @ qr.abs()).max()) / d ** 0.5
+        H8.assert_attention(out[s, t].double().cpu().numpy(), want.cpu().numpy(), size, float(v.abs().max()), fp16=True)
+    L.lorc_destroy(ctx)
+
+
+def test_sizes_that_are_refused():
+    """2^30 tokens in a call, and lists of 2^30 units of 64 tokens for the streaming kernel; nothing of the memory is touched."""
+    import torch
+    L = H.lib()
+    ctx = L.lorc_create(1, 64, 1, 1, 64, 10000.0, max_pos=65536)
+    w = torch.zeros(64, 64, dtype=torch.bfloat16, device="cuda")
+    L.lorc_load_factors(ctx, 0, L.LORC_MODE_FULL, 0, 0, w, None, w, None)
+    some = torch.zeros(4096, dtype=torch.int32, device="cuda")
+    for batch, T, calls in ((1 << 14, 65536, "wp"), (1 << 20, 1, "d"), (1 << 20, 1024, "wp")):
+        cache = L.make_cache8(some, some, some, some, some, batch, 65536, L.LORC_CACHE8_INT8, seq_stride=65536)
+        for c, call in (("w", lambda: L.lorc_append8(ctx, 0, cache, some, T)), ("d", lambda: L.lorc_decode_attn8(ctx, 0, cache, some, some)),
+                        ("p", lambda: L.lorc_prefill_attn8(ctx, 0, cache, some, some, T))):
+            if c in calls:
+                with pytest.raises(L.LorcError) as e:
+                    call()
+                assert e.value.code == L.LORC_ERR_ARG, str(e.value)
+    assert L.lorc_sync_status(ctx) == 0
+    L.lorc_destroy(ctx)
