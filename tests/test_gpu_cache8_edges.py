@@ -170,6 +170,59 @@ def test_chunks_of_the_latent_cache_far_below_the_heaviest():
     L.lorc_destroy(ctx)
 
 
+# (8 KV heads in groups of 1, 4, 6: 128-wide blocks with and without rows that are nobody's; 64-wide ones; what `way` says is by the
+# rules for 148 SMs: streamed, keys shared by all units, by none, by those of the last round)
+MASKS = [((4, 2, 64), 1, [3000, 70], 0), ((32, 8, 128), 1, [2100, 17], 64), ((8, 2, 128), 5, [4000, 5, 130], 16),
+         ((4, 2, 64), 33, [2500, 33], 48), ((32, 8, 128), 150, [5000], 64), ((32, 8, 128), 700, [700], 0),
+         ((64, 8, 128), 300, [300, 4000], 128), ((6, 2, 128), 150, [5000], 0), ((10, 2, 128), 1500, [1500] * 4, 64),
+         ((7, 1, 128), 1500, [1500] * 4, 0), ((32, 8, 64), 150, [5000], 16), ((32, 8, 64), 700, [700], 64),
+         ((64, 8, 64), 300, [300, 4000], 0)]
+
+
+@pytest.mark.parametrize("kind", H8.KINDS)
+@pytest.mark.parametrize("heads,T,lens,page", MASKS)
+def test_masks_to_the_token(kind, heads, T, lens, page):
+    """Keys are zero, so every token that a query sees has the same weight; from the chunk on a token has one number that is not
+    zero, also behind the sequence's end.  A result is a count divided by a length: half a step of the output, and some sums
+    in fp32."""
+    c = H8.Case(kind, *heads, lens, page=page, style=2, seed=70)
+    c.codes[:] = 0.0
+    c.scales[:] = 2.0 ** -3
+    want = np.zeros((c.b, T, heads[2]))
+    for s, n in enumerate(c.lens):
+        room = -(-n // 16) * 16
+        pg, row = c.rows_of(s, room)
+        for pos in range(n - T, room):
+            at = pos % c.d_h
+            c.codes[1][pg[pos], row[pos], at::c.d_h] = 64.0
+            if pos < n:
+                want[s, pos - (n - T):, at] += 8.0
+        want[s] /= np.arange(n - T, n)[:, None] + 1
+    c.upload()
+    q = H.synth.to_bf16_exact(c.rng.standard_normal((c.b, T, c.H_q, c.d_h))).astype(np.float64)
+    got = _attend(c, q, T)
+    off = np.abs(got - want[:, :, None]) - (2.0 ** -8 + 2.0 ** -15) * want[:, :, None]
+    assert off.max() <= 0, np.unravel_index(off.argmax(), off.shape)
+    assert c.L.lorc_last_path(c.ctx) == (2 if T > 100 else 3)
+    assert c.status() == 0 and c.guard_intact()
+    c.close()
+
+
+@pytest.mark.parametrize("kind", H8.KINDS)
+@pytest.mark.parametrize("style", [0, 1])
+@pytest.mark.parametrize("heads,T,lens,page", [m for m in MASKS if m[1] > 100])
+def test_chunks_on_the_tensor_cores(kind, style, heads, T, lens, page):
+    """Every form of the tcgen05 kernel (all units whole, all shared, those of the last round shared; heads of 128 in groups that fill
+    a block or not, interleaved, heads of 64), and that it is the one that runs."""
+    c = H8.Case(kind, *heads, lens, page=page, style=style, theta=500000.0, seed=71)
+    q = H.synth.to_bf16_exact(c.rng.standard_normal((c.b, T, c.H_q, c.d_h))).astype(np.float64)
+    got = _attend(c, q, T)
+    assert c.L.lorc_last_path(c.ctx) == 2 and c.status() == 0 and c.guard_intact()
+    some = np.unique(np.r_[0, 1, T // 2, T - 1, c.rng.integers(0, T, 4)])
+    H8.assert_attention(got[:, some], *c.want_some(q, T, some), fp16=True)
+    c.close()
+
+
 @pytest.mark.parametrize("kind", H8.KINDS)
 @pytest.mark.parametrize("b,T,D,path", [(2, 1, 256, 3), (40, 1, 512, 2), (9, 5, 512, 2), (2, 100, 512, 2), (1, 3, 200, 3)])
 def test_a_write_beside_tokens_under_any_scale(kind, b, T, D, path):
