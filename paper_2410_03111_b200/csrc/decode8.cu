@@ -57,42 +57,11 @@ constexpr float D8_HEAD = 7.f;       // and the heaviest weight then stands at 2
 constexpr float D8_BELOW = 118.f, D8_ABOVE = 125.f;    // how far the reference of the weights may lie from that of the scores
 constexpr float LOG2E = 1.4426950408889634f;
 
-__device__ __forceinline__ void ldmatrix_x4(uint32_t (&r)[4], uint32_t addr) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-                 : "r"(addr)
-                 : "memory");
-}
-__device__ __forceinline__ void ldmatrix_x4_trans(uint32_t (&r)[4], uint32_t addr) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-                 : "r"(addr)
-                 : "memory");
-}
-// transpose of an 8 x 8 matrix of 16-bit elements spread over the warp (row lane / 4, columns 2 (lane % 4), + 1)
-__device__ __forceinline__ uint32_t movmatrix_trans(uint32_t x) {
-    uint32_t y;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
-    return y;
-}
-__device__ __forceinline__ void mma_f16_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
-                                              uint32_t b1) {
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
 __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
     const __half2 v = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 __device__ __forceinline__ float2 unpack_half(uint32_t x) { return __half22float2(*reinterpret_cast<const __half2*>(&x)); }
-// 2^x for x <= D8_RAISE (relative error 2^-22)
-__device__ __forceinline__ float ex2_approx(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 
 // log2 |x| of a scale, -infinity for zero (absolute error below 2^-15, a thirtieth of what a weight loses as an fp16 number)
 __device__ __forceinline__ float d8_log2(float x) { return __log2f(fabsf(x)); }
@@ -157,16 +126,6 @@ struct D8Range {
     int f, end, first, row, per, base;
 };
 
-// Inclusive sums of w over the lanes.
-__device__ __forceinline__ int warp_sums(int w, int lane) {
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int x = __shfl_up_sync(0xffffffffu, w, o);
-        if (lane >= o) w += x;
-    }
-    return w;
-}
-
 // By whole warps.  Up to 128 rows are loaded at once.
 __device__ __forceinline__ D8Range d8_range(const D8Params& p, int part, int lane) {
     D8Range r;
@@ -209,7 +168,7 @@ __device__ __forceinline__ D8Range d8_range(const D8Params& p, int part, int lan
     int before = 0;
     bool found = false;
     auto look = [&](int i0, int x) {             // rows i0 .. i0 + 31, lane's weight x
-        const int end = warp_sums(x, lane);
+        const int end = warp_scan(x, lane);
         const unsigned hit = __ballot_sync(0xffffffffu, r.f < before + end);
         if (hit) {
             const int l = __ffs(hit) - 1;

@@ -41,16 +41,6 @@ __device__ __forceinline__ int held_pages(const PagesView& p, int len) {
     return len <= 0 || !row_fits(p, len) ? 0 : (len - 1) / p.page_size + 1;
 }
 
-// Inclusive sums over the lanes of a warp.
-template <typename T>
-__device__ __forceinline__ T warp_scan(T x, int lane) {
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const T y = __shfl_up_sync(0xffffffffu, x, o);
-        if (lane >= o) x += y;
-    }
-    return x;
-}
 // Sums over the block in thread order: the sum of the threads before this one; `all` receives the sum of all.  (All threads.)
 template <typename T>
 __device__ __forceinline__ T block_scan(T x, T* sums, T& all) {

@@ -346,12 +346,6 @@ struct FaParams {
     float* part_o;                 // SPLIT: [unit][n_split][256 rows][DH] un-normalised output
 };
 
-__device__ __forceinline__ float ex2_approx(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
 // 32 scores of a row -> probabilities 2^(s - m), rounded to fp16 and packed two per column at tensor-memory address
 // taddr (16 columns); their unrounded sums are added to l0 / l1.  (Packed fp32 adds for the subtraction and the sums
 // were measured 2.5 % slower than these scalar ones: the pack / unpack moves cost more than the adds they save.)
