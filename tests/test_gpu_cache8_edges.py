@@ -320,3 +320,100 @@ def test_sizes_that_are_refused():
                 assert e.value.code == L.LORC_ERR_ARG, str(e.value)
     assert L.lorc_sync_status(ctx) == 0
     L.lorc_destroy(ctx)
+
+
+def _step(c, T):
+    """Buffers and calls of a step: a chunk of T tokens is written and attended to, then its last token as a step of its own."""
+    import torch
+    x = H.dev_bf16(c.rng.standard_normal((c.b, T, c.D)))
+    last = x[:, -1:].contiguous()
+    q, qd = c.queries(T, scale=1.0)
+    q1 = qd[:, -1].contiguous()
+    out, dec = torch.zeros_like(qd), torch.zeros_like(q1)
+    cache = c.cache()
+    c.workspace(T)
+
+    def calls():
+        c.L.lorc_append8(c.ctx, 0, cache, x, T)
+        c.L.lorc_prefill_attn8(c.ctx, 0, cache, qd, out, T)
+        c.path = c.L.lorc_last_path(c.ctx)
+        c.L.lorc_append8(c.ctx, 0, cache, last, 1)
+        c.L.lorc_decode_attn8(c.ctx, 0, cache, q1, dec)
+
+    return calls, [out, dec, c.kv, c.sc]
+
+
+@pytest.mark.parametrize("kind", H8.KINDS)
+@pytest.mark.parametrize("T,path", [(3, 3), (150, 2), (700, 2)])
+def test_a_captured_chunk_under_other_lengths(kind, T, path):
+    """One graph, replayed with other lengths (empty, shorter than the chunk, the longest): what the calls give."""
+    import torch
+    c = H8.Case(kind, 32, 8, 128, [T, T + 900, T + 40], page=64, D=512, seed=80, max_len=T + 1000)
+    calls, held = _step(c, T)
+    calls()
+    assert c.path == path and c.status() == 0
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        calls()
+    for lens in ([T, T + 900, T + 40], [T + 17, T + 1000, T], [0, T + 1, T - 1], [T + 500, T + 499, T + 498]):
+        c.sl.copy_(torch.tensor(lens, dtype=torch.int32))
+        kv, sc = c.kv.clone(), c.sc.clone()
+        graph.replay()
+        torch.cuda.synchronize()
+        got, status = [t.clone() for t in held], c.status()
+        c.kv.copy_(kv)
+        c.sc.copy_(sc)
+        for t in held[:2]:
+            t.fill_(7.0)
+        calls()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, held)), lens
+        assert status == c.status() or min(lens) < T        # (of several errors one is kept)
+    assert c.guard_intact()
+    c.close()
+
+
+def test_two_contexts_at_once():
+    """Contexts share nothing: on two streams at the same time they give what they give alone."""
+    import torch
+    cases = [(H8.Case("int8", 32, 8, 128, [150 + 37 * s for s in range(6)], page=64, D=512, seed=81, max_len=600), 150),
+             (H8.Case("e4m3", 12, 6, 64, [40 + s % 90 for s in range(40)], D=1024, seed=82, max_len=200), 5)]
+    steps = [_step(c, T) for c, T in cases]
+    alone = []
+    for calls, held in steps:
+        calls()
+        torch.cuda.synchronize()
+        alone.append([t.clone() for t in held])
+    streams = [torch.cuda.Stream() for _ in cases]
+    graphs = []
+    for (calls, _), stream in zip(steps, streams):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            for _ in range(4):
+                calls()
+        graphs.append(graph)
+    for _ in range(25):
+        for graph, stream in zip(graphs, streams):
+            with torch.cuda.stream(stream):
+                graph.replay()
+    torch.cuda.synchronize()
+    for (_, held), want, (c, _) in zip(steps, alone, cases):
+        assert all(torch.equal(a, b) for a, b in zip(held, want))
+        assert c.status() == 0 and c.guard_intact()
+        c.close()
+
+
+@pytest.mark.parametrize("kind", H8.KINDS)
+def test_chunks_whose_pages_lie_outside_the_pool(kind):
+    """Expanded chunks: such tokens count as zeros (status CAPACITY), the other sequences are as ever."""
+    import torch
+    c = H8.Case(kind, 32, 8, 128, [1500, 400], page=32, seed=83)
+    c.table[0, 2], c.table[0, 40] = -1, 10 ** 6
+    q = H.synth.to_bf16_exact(c.rng.standard_normal((c.b, 200, c.H_q, c.d_h))).astype(np.float64)
+    got = _attend(c, q, 200)
+    assert c.L.lorc_last_path(c.ctx) == 2 and c.status() == c.L.LORC_ERR_CAPACITY and c.guard_intact()
+    for page in (c.table_h[0, 2], c.table_h[0, 40]):
+        c.codes[:, page] = 0.0
+    some = np.array([0, 63, 199])
+    H8.assert_attention(got[:, some], *c.want_some(q, 200, some), fp16=True)
+    c.close()
