@@ -19,6 +19,9 @@ namespace {
 // ---------------------------------------------------------------------------------------------
 // projection for a handful of tokens: grid (2 n / 8, tiles of 16 tokens), eight warps = eight slices of D.  Bound by the stream of
 // the factor (in fragment order, see retile_factor_kernel), which is requested before the kernel in front has finished.
+// The MMAs sum 128 products at a time, and ordinary additions the pieces: an MMA loses more of its running sum than rounding would.
+// (D 8192, products of one sign: off by 2^-19.1 of their sum with 1024 at a time, by 2^-23.3 so; codes that are not the fp64
+// projection's 2.5e-4 and 3e-5.  16 x 1 tokens take as long, 1 x 1 5.40 us instead of 5.33.)
 // ---------------------------------------------------------------------------------------------
 __global__ void __launch_bounds__(256, 2)
 project8_mma_kernel(const bf16* __restrict__ x, const bf16* __restrict__ A_tiled, float* __restrict__ proj, int D, int R,
@@ -63,13 +66,16 @@ project8_mma_kernel(const bf16* __restrict__ x, const bf16* __restrict__ A_tiled
                     if (row_hi) hi[i] = xb[(kb0 + i0 + i) * 4];
                 }
             }
+            float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 if (kb0 + i0 + i < steps) {
-                    mma_bf16_16816(c, lo[i].x, hi[i].x, lo[i].y, hi[i].y, w[i0 + i].x, w[i0 + i].y);
-                    mma_bf16_16816(c, lo[i].z, hi[i].z, lo[i].w, hi[i].w, w[i0 + i].z, w[i0 + i].w);
+                    mma_bf16_16816(part, lo[i].x, hi[i].x, lo[i].y, hi[i].y, w[i0 + i].x, w[i0 + i].y);
+                    mma_bf16_16816(part, lo[i].z, hi[i].z, lo[i].w, hi[i].w, w[i0 + i].z, w[i0 + i].w);
                 }
             }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) c[i] += part[i];
         }
     }
 #pragma unroll

@@ -417,3 +417,29 @@ def test_chunks_whose_pages_lie_outside_the_pool(kind):
     some = np.array([0, 63, 199])
     H8.assert_attention(got[:, some], *c.want_some(q, 200, some), fp16=True)
     c.close()
+
+
+@pytest.mark.parametrize("b", [5, 16])
+def test_sums_of_a_few_tokens(b):
+    """Products of one sign, so that what the tensor cores' fp32 sums lose adds up: every code is the fp64 projection's, unless that lies
+    within 2^-20 of the products' sum of a border between two.  Each of 8 MMAs in a row (128 products) loses an ulp, 2^-23, of
+    their sum so far: 2^-21; eight such pieces per warp are added up in fp32, 2^-22, and those of eight warps, 3 2^-24: together
+    less than 2^-20."""
+    import torch
+    D = 8192
+    for seed in range(3):
+        c = H8.Case("int8", 8, 8, 128, [16] * b, D=D, style=H.ROPE_NONE, seed=seed)
+        w = [H.synth.to_bf16_exact(np.abs(c.rng.standard_normal((D, c.n))) / np.sqrt(D)) for _ in range(2)]
+        c.L.lorc_load_factors(c.ctx, 0, c.L.LORC_MODE_FULL, 0, 0, H.dev_bf16(w[0]), None, H.dev_bf16(w[1]), None)
+        x = H.dev_bf16(H.synth.to_bf16_exact(np.abs(c.rng.standard_normal((b, 1, D)))))
+        c.sc.fill_(2.0 ** -100)
+        c.workspace(1)
+        c.L.lorc_append8(c.ctx, 0, c.cache(), x, 1)
+        assert c.L.lorc_last_path(c.ctx) == 3 and c.status() == 0
+        for i in range(2):
+            new = (x[:, 0].double() @ H.dev_bf16(w[i]).double()).view(b, 8, 128)
+            scale = c.sc[i, :, 0].double()[..., None]
+            got = c.kv[i, :, 15].double().view(b, 8, 128)
+            near = (new / scale - (torch.floor(new / scale) + 0.5)).abs() * scale <= 2.0 ** -20 * new
+            assert bool(((got == torch.round(new / scale)) | near).all())
+        c.close()
