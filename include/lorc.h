@@ -58,7 +58,7 @@ extern "C" {
                                    form of Sec. 3.1 (the W_q' equation), s = (B_K q) . c: keys are never reconstructed */
 
 /* context flags */
-#define LORC_FLAG_DEBUG_FP32 1  /* run the plain fp32 CUDA-core kernels everywhere (debug path) */
+#define LORC_FLAG_DEBUG_FP32 1  /* run the plain fp32 CUDA-core kernels everywhere (debug path; attention over the 8-bit cache has none) */
 #define LORC_FLAG_PROFILE 2     /* bracket every kernel with CUDA events (see lorc_profile_read) */
 
 /* stages reported by lorc_profile_read */
@@ -287,13 +287,15 @@ int lorc_decode_step_host(lorc_ctx* ctx, int layer, const lorc_cache* cache, con
  *     k_scale, ...  [batch][seq_stride / 16][n_kv_heads], or paged [n_pages][page_size / 16][n_kv_heads]
  * Keys are stored rotated at their positions, as in the bf16 cache of these layers.  page_size and seq_stride are
  * multiples of 16, so that a block lies within one page.  seq_lens, max_seq_len and the page table are as in lorc_cache.
- * Attention takes any finite scales; lorc_append8 writes powers of two.  Rows behind a sequence's end, and scales of
+ * Attention takes any finite scales with which scores and weighted sums of values stay within fp32, and lorc_append8 ones under
+ * which earlier tokens stand; it writes powers of two.  Rows behind a sequence's end, and scales of
  * blocks wholly behind it, are neither read into a result nor written.
  * A call has fewer than 2^30 new tokens (batch * T) and, in lorc_decode_attn8, batch * ceil(max_seq_len / 64) below 2^30.
  * A sequence longer than max_seq_len, the capacity or max_pos counts as empty (status CAPACITY); tokens whose page lies
  * outside the pool are left out (CAPACITY too).
- * With LORC_FLAG_DEBUG_FP32 the projection runs on the plain kernel and attention keeps off the tcgen05 kernels (it has no
- * plain form: its products are exact and its sums fp32 in any case).
+ * With LORC_FLAG_DEBUG_FP32 the projection runs on the plain kernel and attention keeps off the tcgen05 kernels; it has no plain
+ * form, and rounds as without the flag: queries to 22 bits, and a token's weight (its probability times the scale of its
+ * values) to fp16, 2^-11 of itself, or 2^-32 of the sequence's heaviest weight; products of these with codes are exact, sums fp32.
  * The calls need a loaded FULL layer and the context's device to be the current one, and like lorc_decode_attn those of one
  * context must not overlap on the GPU: they share its workspace. */
 #define LORC_CACHE8_INT8 0      /* signed integers from -127 to 127 */
@@ -339,9 +341,10 @@ int lorc_decode_attn8(lorc_ctx* ctx, int layer, const lorc_cache8* cache, const 
 /* Attention of the T newest tokens of every sequence, as lorc_prefill_attn, over the 8-bit cache: q, out
  * [batch, T, n_q_heads, d_head] bf16; the T tokens are already cached, and query t sees the tokens up to its own.  A
  * sequence with fewer than T tokens gets zeros, and status ARG (EMPTY if it has none).  Unless
- * there are few queries (or the debug flag is set), keys and values are brought to fp16 in the workspace once per call: code x
- * scale must not exceed 65504 there (status ARG, and what comes of infinities), has steps of 2^-24 below 2^-14, and
- * tokens whose page lies outside the pool count as zeros.
+ * there are few queries (or the debug flag is set), keys and values are brought to fp16 in the workspace once per call, and rotated
+ * queries times log2(e) / sqrt(d_head) as they are read: both have 11 bits, and steps of 2^-24 below 2^-14.  Code x scale must not
+ * exceed 65504 there (status ARG, and what comes of infinities), nor such a query (what comes of infinities); tokens whose
+ * page lies outside the pool count as zeros.
  * Errors: ARG, LAYER, UNSUPPORTED (a compressed layer), WORKSPACE; CAPACITY / EMPTY / ARG through the status word. */
 int lorc_prefill_attn8(lorc_ctx* ctx, int layer, const lorc_cache8* cache, const void* q, void* out, int T, void* stream);
 

@@ -139,7 +139,7 @@ quantize8_kernel(const Append8Params p, const float* __restrict__ proj, int pair
     const int tid = threadIdx.x, r = tid / TPR, d0 = (tid % TPR) * 16;
     const int s = (int)blockIdx.x / p.n_blocks, head = blockIdx.y;
     const bool val = blockIdx.z != 0;
-    // What does not depend on the projection is looked up while that runs (16 x 1 tokens 8.7 us, now 7.3).  Each of its blocks has waited
+    // What does not depend on the projection is looked up while that runs (16 x 1 tokens 8.8 us, now 7.8).  Each of its blocks has waited
     // for the kernels in front of it before it lets this kernel start, and it writes nothing but `proj`; from L2, since what this
     // SM may hold of an earlier kernel's reads is not known to be given up before the wait.
     Append8Row row;
@@ -220,10 +220,12 @@ static long long mma_time(const lorc_ctx* ctx, long long tiles) {
 constexpr long long MMA_TILES = 64;      // (beyond them every way is faster)
 
 // The kernels for a call: those that should take least.  Measured, us, 8 KV heads of 128 dimensions, D 4096 (sequences x tokens), these
-// kernels / D split over clusters / prompts: 1 x 1 5.6 / 8.9 / 21, 16 x 1 7.4 / 9.4 / 21, 32 x 1 11.5 / 9.7 / 22, 64 x 1 19 / 10.4 / 22,
-// 256 x 1 - / 15 / 55, 512 x 1 - / 32 / 118, 64 x 4 62 / 16 / 32, 1 x 48 17 / 11 / 21, 1 x 120 - / 16 / 21, 1 x 250 - / 25 / 22,
-// 16 x 20 - / 48 / 22; D 8192: 16 x 1 10.6 / 12 / 36, 32 x 1 17.9 / 12.2 / 36, 128 x 1 56 / 17 / 52; 32 KV heads: 16 x 1 23.8 / 27.3,
-// 32 x 1 39 / 28; 8 KV heads of 64, D 2048: 16 x 1 5.6 / 6.8, 64 x 1 10.7 / 7.1.
+// kernels / D split over clusters / prompts: 1 x 1 5.4 / 8.8 / 21, 16 x 1 7.8 / 9.3 / 21, 32 x 1 11.8 / 9.5 / 22, 64 x 1 19 / 10.6 / 22,
+// 256 x 1 64 / 16 / 55, 512 x 1 - / 31 / 118, 64 x 4 61 / 16 / 32, 1 x 48 16 / 11 / 21, 1 x 120 35 / 16 / 22, 1 x 250 60 / 25 / 22,
+// 16 x 20 - / 48 / 23; D 8192: 16 x 1 12.3 / 12.3 / 37, 32 x 1 21.7 / 13.2 / 37, 128 x 1 59 / 18 / 52; 32 KV heads: 16 x 1 24 / 27 / 24,
+// 32 x 1 39 / 28 / 33; 8 KV heads of 64, D 2048: 16 x 1 5.5 / 6.8 / 14, 64 x 1 10.0 / 7.1 / 14.
+// (D that is no multiple of 512, or above 8192, has no kernel for split D: batches of single tokens run here once per 16 of
+// them, or on the prompts' kernel with one new row in sixteen.)
 Append8Way lorc_append8_way(const lorc_ctx* ctx, int batch, int T) {
     const long long tiles = ((long long)batch * T + 15) / 16;
     const bool split = lorc_append8_split_supported(ctx, batch, T), tc = lorc_append8_tc_supported(ctx);

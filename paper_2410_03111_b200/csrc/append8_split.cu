@@ -8,7 +8,7 @@
 // scale needs.  Nothing passes through the workspace.
 //
 // Two CTAs fit an SM, not for more in flight but because clusters of eight large ones do not fill the GPU (15 of them, where 16 tiles
-// of columns want to run; the second round doubled the time).  8 KV heads of 128 dimensions, D 4096: 32 tokens 9.5 us, 64 10.4, 256 15.6;
+// of columns want to run; the second round doubled the time).  8 KV heads of 128 dimensions, D 4096: 32 tokens 9.5 us, 64 10.6, 256 15.5;
 // the factor's bytes take 2.6 at the rate of a copy, the rest is the chain of launch, three rounds of loads, two cluster barriers.
 //
 // Rows.  A group of 16 rows holds every number that shares a scale with one of its own: T <= 16 new tokens of 16 / T sequences (a

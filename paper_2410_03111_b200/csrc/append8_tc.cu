@@ -9,7 +9,8 @@
 // stages.  The tensor cores' fp32 sums lose more than rounding would as they grow longer, and a number near the border between
 // two codes may then fall on the other side; so the MMAs sum 512 products at a time, in two accumulators in TMEM by turns, and
 // sixteen epilogue warps add these up in registers.  (D 4096, codes that are not the fp64 projection's: 1.2e-5 of them, as with a
-// plain fp32 projection; with one sum of 4096 1.0e-4, in 7 % less time, with sums of 256 0.6e-5, in 13 % more.)  Rows of a block that
+// plain fp32 projection; with one sum of 4096 1.0e-4, in 7 % less time, with sums of 256 0.6e-5, in 13 % more.  Products of one sign
+// are off by 2^-20.1 of their sum at most.)  Rows of a block that
 // are not new (earlier tokens, or behind the end) lie outside x and read as zero.
 #include <math.h>
 

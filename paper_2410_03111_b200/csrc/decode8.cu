@@ -31,10 +31,10 @@
 // columns; each column has its own last token.  (8 x 4096 tokens, four heads per KV head: 4 queries 31 us, one by one 43; 16
 // queries 90 and 147.)
 //
-// Measured, 8 KV heads of 128 dimensions: 16 x 4129 tokens 30 us (4.5 TB/s), 4 x 32777 49 us (5.5), 64 sequences of 512 to
-// 16384 185 us (6.0; a copy 6.6), 128 x 300 31 us: there it is the 1.5 us per sequence and block from its last tile's
-// arrival to the next one's first products.  (Query fragments made by the queries' warp save 1 us of the 31 and cost 1 of
-// the 13 of 64 x 200.)
+// Measured, 8 KV heads of 128 dimensions: 16 x 4129 tokens 29.4 us (4.6 TB/s), 4 x 32777 48.8 us (5.5), 64 sequences of 512 to
+// 16384 185 us (6.0; a copy 6.6), 202 to 217 (5.1 to 5.5) when calls go on and the power cap lowers the clock, 128 x 300 31 us: there it is the 1.5 us
+// per sequence and block from its last tile's arrival to the next one's first products.  (Query fragments made by the queries'
+// warp save 1 us of the 31 and cost 1 of the 13 of 64 x 200.)
 #include <math.h>
 
 #include "cache8.cuh"
@@ -143,7 +143,11 @@ __device__ __forceinline__ D8Range d8_range(const D8Params& p, int part, int lan
     const int total = __reduce_add_sync(0xffffffffu, sum + w[0] + w[1] + w[2] + w[3]);
     r.per = max((int)((unsigned)(total + p.parts - 1) / (unsigned)p.parts), p.least);
     if (p.each > 0) {
-        // as many parts for every row: each row is a list of its own
+        // As many parts for every row, where that gives no block more than a quarter above the even cut: each row is a list of its
+        // own, no part ends one row and begins the next.  (8 KV heads of 128 dimensions, us, this and the even cut, in brackets the
+        // longest part over the even one: 16 x 1000 14.1 and 17.0, 16 x 4129 29.8 and 32.6, 16 x 16000 85.3 and 87.7 (1.15); 12 x 4129
+        // 24.1 and 27.7 (1.0), 8 x 2000 14.2 and 17.2 (1.14), 32 x 8000 82.6 and 86.5 (1.15), 4 x 16000 29.1 and 31.0 (1.0); two to eight
+        // sequences of 1000 the same.  Beyond: 24 x 1000 15.8 and 20.1, 24 x 4129 45.3 and 41.1, 24 x 8000 80.1 and 68.6 (1.5).)
         const int most = __reduce_max_sync(0xffffffffu, max(max(w[0], w[1]), max(w[2], w[3])));
         const int longest = (int)((unsigned)(most + p.each - 1) / (unsigned)p.each);
         if (longest <= r.per + max(r.per / 4, 2)) {

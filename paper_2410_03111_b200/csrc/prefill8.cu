@@ -1,7 +1,7 @@
 // Prompt chunks over the 8-bit cache of uncompressed layers: keys and values of the cached tokens are brought to fp16 once per
 // call (code x scale has seven significant bits: exact where the scale is a power of two and the number within fp16's normal range),
-// then the tcgen05 attention kernel of the latent mode runs over them.  With T queries per sequence that kernel does 4 T d G products per number of the buffer, so the
-// pass over it is small for chunks.
+// then the tcgen05 attention kernel of the latent mode runs over them.  With T queries per sequence each number of the buffer enters up to
+// T G products, so the pass over it is small for chunks.
 #include <math.h>
 
 #include "cache8.cuh"
@@ -85,8 +85,9 @@ struct Split8 {
 
 // A CTA takes 2.2 us per tile of 128 keys and 4 us before and after, whatever runs beside it; the merge 3 us and its traffic.  Either
 // all units share their keys among S CTAs, or those that the full rounds of the SMs leave over.  (Whole calls, 8 KV heads of 128
-// dimensions in groups of four: 128 tokens behind 8000 took 152 us with one CTA per unit and 48 as chosen here, 512 tokens 150 and
-// 100.  8 x 512 tokens behind 3584, 512 units on 148 SMs: 325 us in four rounds, 311 with the last 68 units shared by two CTAs each.)
+// dimensions in groups of four: the last 128 of 8000 tokens took 144 us with one CTA per unit and 47 as chosen here, 512 of them 146 and
+// 99.  8 x 512 tokens behind 3584, 512 units on 148 SMs: 325 us in four rounds, 309 with the last 68 units shared by two CTAs each; when calls
+// go on for long 3 to 8 % more.)
 Split8 prefill8_split(const lorc_ctx* ctx, int batch, int max_seq_len, int T) {
     const int qp = 2 * (128 / ctx->group);
     const long long P = ctx->sm_count, tiles = ((long long)max_seq_len + 127) / 128;
@@ -118,9 +119,10 @@ size_t expand8_bytes(const lorc_ctx* ctx, int batch, int max_seq_len) {
 
 // Few queries per sequence are better served by the streaming kernel, which reads the codes once per lorc_decode8_queries of them (from
 // L2, mostly) and is then bound by its arithmetic: 0.33 us per 64 tokens, pass and KV head on an SM, against 1.3 us to expand them for
-// all queries.  (8 KV heads of 128 dimensions in groups of four, us here and there: 8 x 4096 tokens, 4 queries 31 and 87, 16 queries
-// 90 and 87, 32 queries 161 and 89; one sequence of 1000 tokens, 32 queries 15 and 20; of 8000, 32 queries 49 and 41.  8 x 512 queries
-// of 4096 tokens, heads of 64 in groups of four, 1513 and 254; heads of 128 in groups of five 4279 and 434, ungrouped 1144 and 231.)
+// all queries.  (8 KV heads of 128 dimensions in groups of four, us here and there: 8 x 4096 tokens, 4 queries 31 and 85, 16 queries
+// 89 and 85, 32 queries 163 and 87; one sequence of 1000 tokens, 32 queries 15 and 18; of 8000, 32 queries 50 and 39.  8 x 512 queries
+// of 4096 tokens 2306 and 309, heads of 64 in groups of four, 1510 and 246; heads of 128 in groups of five 4292 and 432, ungrouped 1171
+// and 226.)
 bool lorc_prefill8_supported(const lorc_ctx* ctx, const Cache8View& cv, int T) {
     if (T == 1 || cv.batch > 65535 || (ctx->desc.flags & LORC_FLAG_DEBUG_FP32)) return false;
     const long long units = (long long)cv.batch * cv.n_kv * ((cv.max_seq_len + 63) / 64), P = ctx->sm_count;
