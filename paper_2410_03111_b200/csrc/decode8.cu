@@ -32,9 +32,9 @@
 // queries 90 and 147.)
 //
 // Measured, 8 KV heads of 128 dimensions: 16 x 4129 tokens 29.4 us (4.6 TB/s), 4 x 32777 48.8 us (5.5), 64 sequences of 512 to
-// 16384 185 us (6.0; a copy 6.6), 202 to 217 (5.1 to 5.5) when calls go on and the power cap lowers the clock, 128 x 300 31 us: there it is the 1.5 us
-// per sequence and block from its last tile's arrival to the next one's first products.  (Query fragments made by the queries'
-// warp save 1 us of the 31 and cost 1 of the 13 of 64 x 200.)
+// 16384 185 us (6.0; a copy 6.6), 202 to 217 (5.1 to 5.5) when calls go on and the power cap lowers the clock, 128 x 300 31 us:
+// there it is the 1.5 us per sequence and block from its last tile's arrival to the next one's first products.  (Query fragments
+// made by the queries' warp save 1 us of the 31 and cost 1 of the 13 of 64 x 200.)
 #include <math.h>
 
 #include "cache8.cuh"

@@ -86,8 +86,8 @@ struct Split8 {
 // A CTA takes 2.2 us per tile of 128 keys and 4 us before and after, whatever runs beside it; the merge 3 us and its traffic.  Either
 // all units share their keys among S CTAs, or those that the full rounds of the SMs leave over.  (Whole calls, 8 KV heads of 128
 // dimensions in groups of four: the last 128 of 8000 tokens took 144 us with one CTA per unit and 47 as chosen here, 512 of them 146 and
-// 99.  8 x 512 tokens behind 3584, 512 units on 148 SMs: 325 us in four rounds, 309 with the last 68 units shared by two CTAs each; when calls
-// go on for long 3 to 8 % more.)
+// 99.  8 x 512 tokens behind 3584, 512 units on 148 SMs: 325 us in four rounds, 309 with the last 68 units shared by two CTAs each; 3 to 8 %
+// more when calls go on and the power cap lowers the clock.)
 Split8 prefill8_split(const lorc_ctx* ctx, int batch, int max_seq_len, int T) {
     const int qp = 2 * (128 / ctx->group);
     const long long P = ctx->sm_count, tiles = ((long long)max_seq_len + 127) / 128;
