@@ -393,7 +393,8 @@ int lorc_pages_free(lorc_ctx* ctx, const lorc_pages* pages, const int32_t* rows,
  * by one) and, where the parent's last page is partly filled, a page of its own with that page's contents, in every array;
  * and it has the parent's length.  So parent and child can both be written to.  The parent's row stays as it is, and may be
  * listed more than once.  A pair is left out, with status ARG, if a row is outside the table, the child is not empty, or
- * the child stands earlier in the list; and with status CAPACITY, its child staying empty, if no free page is left for it. */
+ * the child is that of an earlier pair which none of this (nor its parent's length) leaves out; and with status CAPACITY, its
+ * child staying empty, if no free page is left for it. */
 int lorc_pages_fork(lorc_ctx* ctx, const lorc_pages* pages, const int32_t* parents, const int32_t* children, int n, void* stream);
 
 /* Room for grow[s] more tokens (device int32 [n_rows], <= 0: none) in every row s: takes the pages that this needs, in the
