@@ -373,6 +373,7 @@ cudaError_t lorc_append8_tc_launch(lorc_ctx* ctx, const LorcLayer& L, const Appe
     }
     p.n_units = R / nb;
     const long long total = (long long)p.m_units * p.n_units;
+    if (total > 0x7fffffffll - slots) return cudaErrorInvalidValue;      // (units are counted in 32 bits)
     const int pairs = total < slots ? (int)total : slots;
     const bool two = nb == NB_MAX;
     auto kernel = DH == 128 ? (e4m3 ? (two ? append8_tc_kernel<128, true, 2> : append8_tc_kernel<128, true, 1>)
