@@ -19,7 +19,8 @@
 //                       query row; the probabilities go back into tensor memory as fp16 over the scores  ->  O += P V
 //                       with P read from tensor memory.  The two blocks alternate, so the tensor pipe works on one
 //                       while the other's softmax runs.  The running reference of a row is only raised when a tile
-//                       exceeds it by more than 2^8 (the accumulator is rescaled then), so most tiles need no pass over O.
+//                       exceeds it by more than 2^15 (2^8 above the score that set it; the accumulator is rescaled then), so
+//                       most tiles need no pass over O.
 #include <cuda_fp16.h>
 #include <math.h>
 
@@ -320,9 +321,11 @@ lorc_reconstruct_kernel(const __grid_constant__ CUtensorMap mapCK, const __grid_
 // scores.  Tensor memory: scores / probabilities of block b at column 128 b, its output at column 256 + 128 b.
 constexpr int F_THREADS = 320;       // warp 0 TMA, warp 1 MMA, warps 2..5 softmax of block 0, warps 6..9 of block 1
 constexpr int F_STAGES = 2;
-constexpr float F_RAISE = 8.f;       // a row's reference is raised only when a tile exceeds it by more than this (log2 units)
-constexpr float F_HEAD = 7.f;        // the reference's probability is 2^7, so they reach 2^15 as fp16 numbers, and one below 2^-21 of
-                                     // the largest is off by 2^-32 of that (with 1 for the reference's 2^-25, and smaller ones lost)
+// A row's reference stands 2^F_HEAD below the largest score (log2 units) and is raised only when a tile exceeds it by more than 2^15:
+// probabilities reach 2^15 as fp16 numbers, and one below 2^-21 of the largest is off by 2^-32 of that (with the largest at 1 2^-25,
+// and smaller ones lost).
+constexpr float F_HEAD = 7.f;
+constexpr float F_RAISE = 15.f;
 
 struct FaSmem {
     bf16 Q[2][2][TILE * KC];              // [block][64-element half][128 rows]
@@ -632,7 +635,7 @@ lorc_prefill_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_
             const bool raise = mt > m_ref + F_RAISE || (m_ref == -INFINITY && mt > -INFINITY);
             if (__any_sync(0xffffffffu, raise)) {
                 // what has been accumulated so far shrinks by 2^(old - new)
-                const float alpha = !raise ? 1.f : (m_ref == -INFINITY ? 0.f : exp2f(m_ref - mt));
+                const float now = mt - F_HEAD, alpha = !raise ? 1.f : (m_ref == -INFINITY ? 0.f : exp2f(m_ref - now));
                 l0 *= alpha;
                 l1 *= alpha;
                 if (j > 0) {
@@ -646,11 +649,10 @@ lorc_prefill_attn_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_
                         tmem_st16(orow + c0, o);
                     }
                 }
-                if (raise) m_ref = mt;
+                if (raise) m_ref = now;
             }
-            // probabilities (times 2^F_HEAD, as their sum: at most 2^15), rounded to fp16, packed two per column over the scores
-            // they came from
-            const float m_use = m_ref == -INFINITY ? 0.f : m_ref - F_HEAD;     // a row that has seen nothing yet: 2^(-inf) = 0
+            // probabilities (at most 2^15), rounded to fp16, packed two per column over the scores they came from
+            const float m_use = m_ref == -INFINITY ? 0.f : m_ref;     // a row that has seen nothing yet: 2^(-inf) = 0
             probs_chunk(r0, m_use, trow, l0, l1);
             probs_chunk(r1, m_use, trow + 16, l0, l1);
             tmem_wait_st();
